@@ -1,10 +1,11 @@
 """Build the HIP library ``libspec_verify.so`` for gfx950 in-tree with hipcc.
 
-The kernel source is compiled in two passes so that each pass gets only the
+A kernel source is compiled in two passes so that each pass gets only the
 flags meant for it: the device pass (``--cuda-device-only``) is built with
 packed-fp32 instruction formation disabled, and its fat binary is embedded
 into the host pass (``--cuda-host-only``).  Both passes and the host-only
-decoding loop build with ``-Wall -Wextra -Werror``.
+decoding loop build with ``-Wall -Wextra -Werror``.  The sources are compiled
+side by side.
 """
 from __future__ import annotations
 
@@ -13,6 +14,7 @@ import shutil
 import subprocess
 import sys
 import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG_DIR)
@@ -21,8 +23,10 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB_NAME = "libspec_verify.so"
 LIB_PATH = os.path.join(PKG_DIR, LIB_NAME)
 KERNEL_SOURCE = os.path.join(CSRC, "spec_verify.hip")
+CACHE_SOURCES = [os.path.join(CSRC, "cache.hip"), os.path.join(CSRC, "cache_attend.hip")]
+KERNEL_SOURCES = [KERNEL_SOURCE, *CACHE_SOURCES]
 HOST_SOURCES = [os.path.join(CSRC, "decode_loop.hip")]
-SOURCES = [KERNEL_SOURCE, *HOST_SOURCES]
+SOURCES = [*KERNEL_SOURCES, *HOST_SOURCES]
 ARCH = "gfx950"
 
 COMMON_FLAGS = ["-O3", "-std=c++17", "-Wall", "-Wextra", "-Werror"]
@@ -53,20 +57,28 @@ def _run(cmd, verbose: bool) -> None:
         sys.stderr.write(res.stderr)
 
 
+def _compile_kernels(src: str, tmpdir: str, flags, verbose: bool) -> str:
+    name = os.path.splitext(os.path.basename(src))[0]
+    fatbin, obj = os.path.join(tmpdir, name + ".hipfb"), os.path.join(tmpdir, name + ".o")
+    _run([hipcc(), *COMMON_FLAGS, *DEVICE_FLAGS, *flags, "-c", src, "-o", fatbin], verbose)
+    _run([hipcc(), *COMMON_FLAGS, *HOST_FLAGS, *flags, "-Xclang", "-fcuda-include-gpubinary", "-Xclang", fatbin, "-c",
+          src, "-o", obj], verbose)
+    return obj
+
+
+def _compile_host(src: str, tmpdir: str, flags, verbose: bool) -> str:
+    obj = os.path.join(tmpdir, os.path.splitext(os.path.basename(src))[0] + ".o")
+    _run([hipcc(), *COMMON_FLAGS, *HOST_FLAGS, *flags, "-c", src, "-o", obj], verbose)
+    return obj
+
+
 def build(verbose: bool = False, extra_flags=None) -> str:
     """Compile the library; returns its path.  Always recompiles."""
-    inc = ["-I", INCLUDE, "-I", CSRC]
-    extra = list(extra_flags or [])
-    with tempfile.TemporaryDirectory(prefix="sv_build_") as tmpdir:
-        fatbin = os.path.join(tmpdir, "spec_verify.hipfb")
-        objs = [os.path.join(tmpdir, "spec_verify.o")]
-        _run([hipcc(), *COMMON_FLAGS, *DEVICE_FLAGS, *extra, *inc, "-c", KERNEL_SOURCE, "-o", fatbin], verbose)
-        _run([hipcc(), *COMMON_FLAGS, *HOST_FLAGS, *extra, *inc, "-Xclang", "-fcuda-include-gpubinary",
-              "-Xclang", fatbin, "-c", KERNEL_SOURCE, "-o", objs[0]], verbose)
-        for src in HOST_SOURCES:
-            obj = os.path.join(tmpdir, os.path.splitext(os.path.basename(src))[0] + ".o")
-            _run([hipcc(), *COMMON_FLAGS, *HOST_FLAGS, *extra, *inc, "-c", src, "-o", obj], verbose)
-            objs.append(obj)
+    flags = [*(extra_flags or []), "-I", INCLUDE, "-I", CSRC]
+    with tempfile.TemporaryDirectory(prefix="sv_build_") as tmpdir, ThreadPoolExecutor(len(SOURCES)) as pool:
+        jobs = [pool.submit(_compile_kernels, src, tmpdir, flags, verbose) for src in KERNEL_SOURCES]
+        jobs += [pool.submit(_compile_host, src, tmpdir, flags, verbose) for src in HOST_SOURCES]
+        objs = [j.result() for j in jobs]
         tmp = LIB_PATH + ".tmp"
         _run([hipcc(), "-shared", "-fPIC", *objs, "-o", tmp], verbose)
         os.replace(tmp, LIB_PATH)

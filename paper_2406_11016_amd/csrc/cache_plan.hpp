@@ -1,0 +1,156 @@
+// Host planning of the key/value cache's operators: argument checks, the
+// attention's split into tasks and its workspace.  No GPU needed.
+#pragma once
+
+#include <limits.h>
+#include <stddef.h>
+#include <stdint.h>
+
+#include <initializer_list>
+
+#include "spec_cache.h"
+
+namespace sv {
+
+// batch * max_new up to which the plan's one workgroup writes the slots itself.
+constexpr int64_t kPlanOwnSlots = 8192;
+
+constexpr uint32_t kAppendBlocks = 8192;
+
+inline bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+
+inline bool strides_ok(const int64_t (&s)[3]) {
+    for (int64_t x : s)
+        if (x < 0 || x % 8 != 0) return false;
+    return true;
+}
+
+inline bool page_size_ok(int32_t p) { return p >= 16 && p <= 1024 && (p & (p - 1)) == 0; }
+
+inline int32_t page_shift(int32_t p) { return __builtin_ctz((unsigned)p); }
+
+// Slots, table places and a sequence's tokens all fit an int32.
+inline bool cache_table_sizes_ok(int32_t batch, int32_t max_pages, int32_t num_pages, int32_t page_size) {
+    return batch >= 1 && batch <= SV_CACHE_MAX_BATCH && max_pages >= 1 && num_pages >= 1 && page_size_ok(page_size) &&
+           (int64_t)num_pages * page_size <= INT_MAX && (int64_t)max_pages * page_size <= INT_MAX &&
+           (int64_t)batch * max_pages <= INT_MAX;
+}
+
+inline sv_status_t check_cache(sv_dtype_t dtype, int32_t batch, int32_t max_new, int32_t kv_heads, int32_t head_dim,
+                               int32_t num_pages, int32_t page_size, int64_t page_stride) {
+    if (dtype != SV_F16 && dtype != SV_BF16) return SV_ERR_DTYPE;
+    if (batch < 1 || batch > SV_CACHE_MAX_BATCH || max_new < 1 || (int64_t)batch * max_new > INT_MAX || kv_heads < 1 ||
+        kv_heads > 65536 || head_dim < 8 || head_dim > 4096 || head_dim % 8 != 0 || num_pages < 1 ||
+        !page_size_ok(page_size) || (int64_t)num_pages * page_size > INT_MAX)
+        return SV_ERR_SHAPE;
+    if (page_stride < (int64_t)kv_heads * page_size * head_dim || page_stride % 8 != 0) return SV_ERR_PARAM;
+    return SV_OK;
+}
+
+// ---------------------------------------------------------------------------
+// attention
+// ---------------------------------------------------------------------------
+
+// Keys of a unit of work: what a workgroup holds of K and V at a time.
+constexpr int kAttendKeys = 128;
+
+// How a call's work is cut (see cache_attend.hip).
+struct AttendPlan {
+    // joined: a task runs over the prefix and then over its sequence's keys, and
+    // only tasks cut by a workgroup's border have parts.  Otherwise the prefix
+    // has tasks of its own, for the rows of the whole batch.
+    bool joined;
+    int32_t own_rows, own_tiles;  // rows of a sequence's own task (32, 64 or 128); tasks a key/value head
+    int32_t prefix_rows;          // rows of a prefix task
+    int32_t groups;               // workgroups
+    int64_t own_parts, rows;      // row places of the parts: of the first own one, of all
+    size_t cum_bytes;             // one array of sums over the batch
+};
+
+inline bool head_dim_ok(int32_t d) { return d == 64 || d == 80 || d == 96 || d == 128 || d == 256; }
+
+// Rows of a task: 32 for each wave that has rows of its own.  At head_dim 256 two
+// waves of the four: four would need more registers than there are.
+inline int32_t task_rows(int64_t rows, int32_t head_dim) {
+    return rows <= 32 ? 32 : rows <= 64 || head_dim > 128 ? 64 : 128;
+}
+
+// Rows of one sequence from which its tasks run over the prefix themselves:
+// their row tiles are nearly full, so that sharing would save nothing and its
+// parts would still be written and read.
+constexpr int64_t kJoinedRows = 512;
+
+inline AttendPlan attend_plan(int32_t batch, int32_t max_new, int32_t q_heads, int32_t kv_heads, int32_t head_dim,
+                              bool prefix) {
+    AttendPlan p{};
+    const int64_t group = q_heads / kv_heads, rows = max_new * group;
+    p.joined = !prefix || rows >= kJoinedRows;
+    p.own_rows = task_rows(rows, head_dim);
+    p.own_tiles = (int32_t)((rows + p.own_rows - 1) / p.own_rows);
+    p.prefix_rows = task_rows(batch * rows, head_dim);
+    p.groups = head_dim > 128 ? 256 : 512;  // what the 256 CUs hold at a time: one of 128 KiB LDS each, or two of 64
+    if (p.joined) {
+        p.own_parts = 0;
+        p.rows = 2 * (int64_t)p.groups * p.own_rows;
+    } else {
+        const int64_t prefix_tasks = kv_heads * ((batch * rows + p.prefix_rows - 1) / p.prefix_rows);
+        p.own_parts = (prefix_tasks + p.groups) * p.prefix_rows;
+        p.rows = p.own_parts + ((int64_t)batch * kv_heads * p.own_tiles + p.groups) * p.own_rows;
+    }
+    p.cum_bytes = (sizeof(int32_t) * ((size_t)batch + 1) + 255) / 256 * 256;
+    return p;
+}
+
+inline bool attend_sizes_ok(int32_t batch, int32_t max_new, int32_t q_heads, int32_t kv_heads, int32_t head_dim) {
+    return batch >= 1 && batch <= SV_CACHE_MAX_BATCH && max_new >= 1 && kv_heads >= 1 && q_heads >= kv_heads &&
+           q_heads <= 65536 && q_heads % kv_heads == 0 && head_dim_ok(head_dim) &&
+           (int64_t)batch * max_new <= INT_MAX && (int64_t)batch * max_new * q_heads <= INT_MAX;
+}
+
+// The numbers of units fit 31 bits at the longest sequences that the table can name.
+inline bool attend_units_ok(const sv_cache_attend_desc_t& d, const AttendPlan& p) {
+    const int64_t pre = ((int64_t)d.prefix_len + kAttendKeys - 1) / kAttendKeys;
+    const int64_t own = ((int64_t)d.max_pages * d.page_size + kAttendKeys - 1) / kAttendKeys;
+    const double tiles = (double)d.batch * d.kv_heads * p.own_tiles;
+    const double rows = (double)d.batch * d.max_new * (d.q_heads / d.kv_heads);
+    const double pooled = p.joined ? 0.0 : d.kv_heads * (double)pre * (rows / p.prefix_rows + 1.0);
+    return tiles * (double)(own + (p.joined ? pre : 0)) + pooled < 2147483647.0;
+}
+
+inline size_t attend_workspace_bytes(int32_t batch, int32_t max_new, int32_t q_heads, int32_t kv_heads,
+                                     int32_t head_dim) {
+    if (!attend_sizes_ok(batch, max_new, q_heads, kv_heads, head_dim)) return 0;
+    size_t most = 0;
+    for (const bool prefix : {false, true}) {
+        const AttendPlan p = attend_plan(batch, max_new, q_heads, kv_heads, head_dim, prefix);
+        const size_t n = 2 * p.cum_bytes + (size_t)p.rows * ((size_t)head_dim + 2) * sizeof(float);
+        if (n > most) most = n;
+    }
+    return (most + 255) / 256 * 256;
+}
+
+inline sv_status_t check_attend(const sv_cache_attend_desc_t& d) {
+    if (d.q == nullptr || d.out == nullptr || d.k_cache == nullptr || d.v_cache == nullptr || d.block_table == nullptr ||
+        d.lengths == nullptr || d.workspace == nullptr || (d.prefix_len != 0 && d.prefix_table == nullptr))
+        return SV_ERR_NULL;
+    const sv_status_t st = check_cache(d.dtype, d.batch, d.max_new, d.kv_heads, d.head_dim, d.num_pages, d.page_size,
+                                       d.page_stride);
+    if (st != SV_OK) return st;
+    if (!attend_sizes_ok(d.batch, d.max_new, d.q_heads, d.kv_heads, d.head_dim) || d.max_pages < 1 ||
+        (int64_t)d.batch * d.max_pages > INT_MAX || (int64_t)d.max_pages * d.page_size > INT_MAX || d.prefix_len < 0 ||
+        (int64_t)d.prefix_len + (int64_t)d.max_pages * d.page_size > INT_MAX)
+        return SV_ERR_SHAPE;
+    if (!attend_units_ok(d, attend_plan(d.batch, d.max_new, d.q_heads, d.kv_heads, d.head_dim, d.prefix_len > 0)))
+        return SV_ERR_SHAPE;
+    // (scale * log2(e) and its inverse have to be finite)
+    if (!(d.scale > 1e-30f && d.scale < 1e30f)) return SV_ERR_PARAM;
+    if (!aligned16(d.q) || !aligned16(d.out) || !aligned16(d.k_cache) || !aligned16(d.v_cache) ||
+        !strides_ok(d.q_stride) || !strides_ok(d.out_stride))
+        return SV_ERR_PARAM;
+    if (!aligned16(d.workspace) ||
+        d.workspace_bytes < attend_workspace_bytes(d.batch, d.max_new, d.q_heads, d.kv_heads, d.head_dim))
+        return SV_ERR_WORKSPACE;
+    return SV_OK;
+}
+
+}  // namespace sv

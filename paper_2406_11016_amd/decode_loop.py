@@ -28,6 +28,14 @@ streaming an element's rows at its first rejection, Sec. 3.1) or ``"auto"``:
 the early exit when the previous step's mean accepted length was below half
 of its gamma, the single pass otherwise and at the first step.  Both give
 the same outputs.
+
+A target model's key/value cache goes along with ``cache`` (a
+:class:`~paper_2406_11016_amd.paged_cache.PagedCache`): before each iteration's
+producer runs, the loop plans the cache entries of its gamma + 1 tokens a
+sequence, keeping what the last iteration accepted -- one launch on the loop's
+stream, from the accepted lengths where they are.  The producer writes and reads
+the cache through ``loop.cache`` (``append``, ``attend``, ``positions``).  The
+first iteration keeps everything that the program planned before (its prompts).
 """
 from __future__ import annotations
 
@@ -39,6 +47,7 @@ import torch
 
 from . import binding
 from .binding import STORAGE_TORCH_DTYPES
+from .paged_cache import PagedCache
 
 
 def next_gamma(gamma: int, accepted: np.ndarray, gamma_max: int, grow: int = 2, shrink: int = 1) -> int:
@@ -77,7 +86,7 @@ class DecodeLoop:
     def __init__(self, batch: int, vocab: int, dtype: str, *, mode: str = "exact", temperature: float = 1.0,
                  alpha: float = -1.0e4, beta: float = 1.0e4, gamma0: int = 5, gamma_max: int = 20,
                  use_graphs: bool = False, native: bool = False, early_exit: str = "never",
-                 adapt_gamma: bool = True, device="cuda"):
+                 adapt_gamma: bool = True, cache: Optional[PagedCache] = None, device="cuda"):
         if not (1 <= gamma0 <= gamma_max):
             raise ValueError("need 1 <= gamma0 <= gamma_max")
         if early_exit not in EARLY_EXIT_CODES:
@@ -91,6 +100,13 @@ class DecodeLoop:
         self.temperature, self.alpha, self.beta = temperature, alpha, beta
         self.gamma0, self.gamma_max, self.use_graphs = gamma0, gamma_max, use_graphs
         self.device = torch.device(device)
+        if cache is not None and (cache.batch != batch or cache.max_new < gamma_max + 1 or
+                                  cache.device.type != self.device.type or
+                                  self.device.index not in (None, cache.device.index)):
+            raise ValueError(f"the cache must serve {batch} sequences and {gamma_max + 1} new tokens on {self.device}; "
+                             f"it has {cache.batch}, {cache.max_new} on {cache.device}")
+        self.cache = cache
+        self._keep_all = True   # the next iteration keeps all that was planned last (not: what it accepted)
         tdt = STORAGE_TORCH_DTYPES[dtype]
         B, G, V = batch, gamma_max, vocab
         self.draft = torch.empty(B * G * V, dtype=tdt, device=self.device)
@@ -198,6 +214,18 @@ class DecodeLoop:
             binding.init_workspace(self.ws)
         self.stream.synchronize()
 
+    # -- the target model's cache ----------------------------------------------
+    def plan_cache(self, gamma: int) -> None:
+        """Enqueue the plan of an iteration's gamma + 1 tokens a sequence (run() does it before each producer)."""
+        with torch.cuda.stream(self.stream):
+            self.cache.plan(gamma + 1, accepted_len=None if self._keep_all else self.acc)
+        self._keep_all = False
+
+    def program_planned(self) -> None:
+        """Between runs, after the program has planned for itself with ``accepted_len=loop.acc`` (new sequences'
+        prompts, say): the next iteration keeps all the tokens of that plan."""
+        self._keep_all = True
+
     def run(self, producer, iterations: int, stats: Optional[LoopStats] = None,
             time_device: bool = False) -> LoopStats:
         """``iterations`` rounds of: producer(self, i, gamma) fills the buffers
@@ -207,6 +235,8 @@ class DecodeLoop:
         gamma = self.gamma0
         ev = (torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)) if time_device else None
         for i in range(iterations):
+            if self.cache is not None:
+                self.plan_cache(gamma)
             producer(self, i, gamma)
             if self.native is not None:
                 nxt_gamma = binding.loop_step(self.native, gamma)
