@@ -13,6 +13,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "cache_split.hpp"
 #include "spec_cache.h"
 
@@ -22,6 +24,7 @@ namespace {
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef short i16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x8 __attribute__((ext_vector_type(8)));
@@ -67,7 +70,7 @@ struct AttendArgs {
     Split split;
     // workspace
     int32_t* cum_tokens;  // [batch + 1] tokens before each sequence
-    uint32_t* cum_units;  // [batch + 1] units before each sequence's own
+    uint32_t* cum_cost;   // [batch + 1] cost of the own tasks before each sequence's
     float* part_out;      // parts: rows x head_dim, fp32
     float* part_max;      // maximum (scores in log2 units)
     float* part_sum;
@@ -89,22 +92,47 @@ __device__ __forceinline__ float halves_sum(float x) {
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// Sums over the batch before each sequence: tokens and units, [batch + 1] each.
-// Every workgroup makes them for itself (a few loads and one scan).
-__device__ __forceinline__ Totals sum_batch(const Split& a, int32_t* cum_tokens, uint32_t* cum_units,
-                                            uint32_t (*wave_sums)[2]) {
+// The batch in LDS: sums over it before each sequence, and its lengths (-1: bad).
+struct Batch {
+    int32_t* cum_tokens;  // [batch + 1]
+    uint32_t* cum_cost;   // [batch + 1]
+    int32_t* lengths;     // [batch]
+};
+__device__ __forceinline__ Sequence sequence(const Batch& batch, int32_t b) {
+    const int32_t length = uniform(batch.lengths[b]);
+    return Sequence{uniform(batch.cum_tokens[b + 1]) - uniform(batch.cum_tokens[b]), max(length, 0), length < 0};
+}
+
+// Every workgroup sums the batch for itself (a few loads and one scan).
+__device__ __forceinline__ Totals sum_batch(const Split& a, const Batch& batch, uint32_t (*wave_sums)[2]) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int each = (a.batch + kThreads - 1) / kThreads;
     const int b0 = min(tid * each, a.batch), b1 = min(b0 + each, a.batch);
-    uint32_t tokens = 0, units = 0;
+    if (a.plan.own_tiles > 4) {  // a wave a sequence, its row tiles by lane
+        for (int b = uniform(wave); b < a.batch; b += kThreads / 64) {
+            const Sequence s = sequence(a, b);
+            uint32_t cost = 0;
+            for (int32_t rt = lane; rt < a.plan.own_tiles; rt += 64) cost += tile_cost(a, s, rt);
+#pragma unroll
+            for (int m = 1; m < 64; m <<= 1) cost += __shfl_xor(cost, m);
+            if (lane == 0) batch.cum_cost[b + 1] = cost;
+        }
+        __syncthreads();
+    }
+    uint32_t tokens = 0, cost = 0;
     for (int b = b0; b < b1; ++b) {
         const Sequence s = sequence(a, b);
         tokens += s.count;
-        units += sequence_units(a, s) * (uint32_t)a.kv_heads;
-        cum_tokens[b + 1] = tokens;
-        cum_units[b + 1] = units;
+        if (a.plan.own_tiles > 4) {
+            cost += batch.cum_cost[b + 1] * (uint32_t)a.kv_heads;
+        } else {
+            for (int32_t rt = 0; rt < a.plan.own_tiles; ++rt) cost += tile_cost(a, s, rt) * (uint32_t)a.kv_heads;
+        }
+        batch.cum_tokens[b + 1] = tokens;
+        batch.cum_cost[b + 1] = cost;
+        batch.lengths[b] = s.bad ? -1 : s.length;
     }
-    uint32_t t = tokens, u = units;
+    uint32_t t = tokens, u = cost;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
         const uint32_t ot = __shfl_up(t, d), ou = __shfl_up(u, d);
@@ -118,30 +146,32 @@ __device__ __forceinline__ Totals sum_batch(const Split& a, int32_t* cum_tokens,
         wave_sums[wave][1] = u;
     }
     __syncthreads();
-    uint32_t bt = t - tokens, bu = u - units;
+    uint32_t bt = t - tokens, bu = u - cost;
     for (int w = 0; w < wave; ++w) {
         bt += wave_sums[w][0];
         bu += wave_sums[w][1];
     }
     for (int b = b0; b < b1; ++b) {
-        cum_tokens[b + 1] += bt;
-        cum_units[b + 1] += bu;
+        batch.cum_tokens[b + 1] += bt;
+        batch.cum_cost[b + 1] += bu;
     }
     if (tid == 0) {
-        cum_tokens[0] = 0;
-        cum_units[0] = 0;
+        batch.cum_tokens[0] = 0;
+        batch.cum_cost[0] = 0;
     }
     __syncthreads();
-    return totals(a, uniform(cum_tokens[a.batch]), uniform(cum_units[a.batch]));
+    return totals(a, uniform(batch.cum_tokens[a.batch]), uniform(batch.cum_cost[a.batch]));
 }
 
-// A sequence's own task that holds its unit `at` of one key/value head: its row
-// tile, and the unit at which it starts.  64 tiles at a time, one a lane.
+// A sequence's own task that holds place `at` of the cost of one key/value head: its
+// row tile, and where its cost starts.  64 tiles at a time, one a lane.
 __device__ __forceinline__ int32_t find_tile(const Split& a, const Sequence& s, uint32_t at, uint32_t& start) {
+    start = 0;
+    if (a.plan.own_tiles == 1) return 0;
     const int lane = threadIdx.x & 63;
     uint32_t before = 0;
     for (int32_t base = 0; base < a.plan.own_tiles; base += 64) {
-        const uint32_t own = (base + lane < a.plan.own_tiles) ? tile_units(a, s, base + lane) : 0u;
+        const uint32_t own = (base + lane < a.plan.own_tiles) ? tile_cost(a, s, base + lane) : 0u;
         uint32_t end = own;
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
@@ -156,19 +186,21 @@ __device__ __forceinline__ int32_t find_tile(const Split& a, const Sequence& s, 
         }
         before += (uint32_t)__builtin_amdgcn_readlane((int)end, 63);
     }
-    start = before;
-    return a.plan.own_tiles - 1;  // (not reached: `at` is below the sum of all tiles)
+    return 0;  // (not reached: `at` is below the sum of all tiles)
 }
 
-// The task of unit u, in scalar registers.
-__device__ __forceinline__ Segment task_at(const Split& a, const Totals& t, const uint32_t* cum_units, uint32_t u) {
-    Segment g = locate(a, t, cum_units, u, [&](const Sequence& s, uint32_t at, uint32_t& start) {
+// The task at place u of the cost, in scalar registers.
+template <class SequenceOf>
+__device__ __forceinline__ Segment task_at(const Split& a, const Totals& t, const uint32_t* cum_cost, uint32_t u,
+                                           SequenceOf sequence_of) {
+    Segment g = locate(a, t, cum_cost, u, sequence_of, [&](const Sequence& s, uint32_t at, uint32_t& start) {
         return find_tile(a, s, at, start);
     });
     g.task = uniform(g.task);
     g.task_start = uniform(g.task_start);
     g.units = uniform(g.units);
     g.prefix_units = uniform(g.prefix_units);
+    g.offset = uniform(g.offset);
     g.kv_head = uniform(g.kv_head);
     g.b = uniform(g.b);
     g.row0 = uniform(g.row0);
@@ -187,10 +219,11 @@ struct Shape {
     static constexpr int kPitch = D <= 64 ? 64 : D <= 128 ? 128 : 256;  // elements of a row in LDS
     static constexpr int kChunks = kPitch / 8;                         // of 16 bytes
     static constexpr int kTile = kKeys * kPitch * 2;                   // bytes of a tile of K or of V
+    static constexpr int kStage = 2 * kTile;                           // of both
     static constexpr int kSteps = D / 16;                              // products over head_dim
     static constexpr int kOuts = (D + 31) / 32;                        // 32-wide pieces of the output
     static constexpr int kRowsLoad = 1024 / (kPitch * 2);              // rows of one wave-wide load
-    static constexpr int kLoads = 32 / kRowsLoad;                      // loads of a wave for its 32 rows
+    static constexpr int kLoads = 16 / kRowsLoad;                      // loads of a wave for its run of 16 rows
 };
 
 // Rows of K and V lie in LDS with their 16-byte chunks permuted by the row, so
@@ -213,12 +246,36 @@ __device__ __forceinline__ void load_to_lds(uint32_t lds, const void* base, uint
                  : "s"(lds), "v"(offset), "s"(base)
                  : "memory");
 }
-template <int N>
-__device__ __forceinline__ void wait_loads() {
-    asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
+// Own loads to LDS have landed, own LDS reads are done; then the workgroup's
+// barrier.  (The wait is the compiler's own instruction, so that it knows that
+// nothing is in flight: it would else wait for the next unit's loads where it
+// first needs a register that was loaded before the loop.)
+__device__ __forceinline__ void stage_barrier() {
+    asm volatile("" : : : "memory");
+    __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" : : : "memory");
 }
-// Own LDS reads done, then the workgroup's barrier.
-__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory"); }
+
+// The same value, of which the compiler knows nothing: what is computed from it is
+// computed there, not kept in registers from before.
+__device__ __forceinline__ int forget(int x) {
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
+// Nothing is moved across: the reads written before a block of matrix products are
+// issued before it, so that their latency passes behind it.
+__device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }
+
+// Own LDS accesses are done; then the workgroup's barrier.  (Loads and stores of
+// memory stay under way.)
+__device__ __forceinline__ void lds_barrier() {
+    asm volatile("" : : : "memory");
+    __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" : : : "memory");
+}
 
 // Whether this thread's share of a tile holds infinities or NaN; `clear` makes them zeros.
 template <class T, int D>
@@ -226,7 +283,7 @@ __device__ __forceinline__ int special_chunks(char* tile, bool clear) {
     using S = Shape<D>;
     uint32_t found = 0;
 #pragma unroll 1
-    for (int at = threadIdx.x * 16; at < S::kTile; at += kThreads * 16) {
+    for (int at = forget(threadIdx.x) * 16; at < S::kTile; at += kThreads * 16) {
         // (a chunk behind head_dim holds what was there before: nothing reads it)
         if (D != S::kPitch && (((at / 16) % S::kChunks) ^ swizzle<D>(at / (S::kPitch * 2))) * 8 >= D) continue;
         u32x4 x = *(u32x4*)(tile + at);
@@ -243,8 +300,10 @@ __device__ __forceinline__ int special_chunks(char* tile, bool clear) {
     return (int)found;
 }
 
-// The part of a task's rows over a run of its units.  Four waves: WR of them
-// split the rows (32 each), 4 / WR the 32-key blocks of a unit.
+// The part of a task's rows over a run of its units.  The four waves are WR x WK x
+// WD: WR split the rows (32 each), WK a unit's blocks of 32 keys, and WD the
+// output's head_dim (those do the same scores twice; it is for tasks of few rows,
+// which wait for memory).
 //
 // The products are taken transposed.  S^T = K Q^T leaves a query row's scores in
 // the registers of two lanes (l and l + 32), so the maximum and the sum over the
@@ -252,88 +311,112 @@ __device__ __forceinline__ int special_chunks(char* tile, bool clear) {
 // rescaling of the output are one value a lane.  P^T then is the B operand of
 // O^T = V^T P^T as it stands (after rounding to the storage type), with V^T from
 // LDS by transposing reads in the same order of keys.
+//
+// K runs one unit ahead of V: while one unit's scores become weights, on the
+// vector units, the matrix units make the next one's scores, product by product in
+// between (the two overlap in one wave only if its instructions alternate).  Both
+// are staged two deep in LDS, with one barrier between units.
 template <class T, int D, int WR>
 __device__ void segment(const AttendArgs& a, const Segment& g, const int32_t* cum_tokens, char* smem,
                         float (*wave_stats)[2][32], int* poison_flag, bool whole, int64_t place) {
     using S = Shape<D>;
     using V8 = typename T::V8;
-    constexpr int WK = 4 / WR, NS = 4 / WK;
-    const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
+    constexpr int WK = WR == 4 ? 1 : 2, WD = 4 / (WR * WK);
+    constexpr int NS = 2 / WK;                        // blocks of 32 keys of a wave
+    constexpr int kPieces = (S::kOuts + WD - 1) / WD;  // pieces of the output of a wave: every WD-th
+    constexpr int kMmas = NS * S::kSteps;              // products of a unit's scores
+    constexpr int kAhead = kMmas < 4 ? kMmas : 4;      // those of them whose reads of K are under way
+    constexpr int kMmasV = 2 * NS * kPieces, kAheadV = kMmasV < 4 ? kMmasV : 4;  // the same of the output and V
+    // (`lane` is forgotten where a part of the work begins: what is made from it there would else be kept in registers
+    // from before the loops on)
+    const int tid = threadIdx.x, lane = forget(tid & 63), half = lane >> 5;
     const int wave = uniform(tid >> 6);
-    const int wr = wave % WR, wk = wave / WR;
-    const uint32_t lds_k = (uint32_t)(uintptr_t)(SV_LDS char*)smem, lds_v = lds_k + S::kTile;
+    const int wr = wave % WR, wk = wave / WR % WK, wd = wave / (WR * WK);
+    const uint32_t lds = (uint32_t)(uintptr_t)(SV_LDS char*)smem;
 
     // the row of this lane
-    const int row = g.row0 + wr * 32 + (lane & 31);
-    int b = g.b, token = 0, head = 0;
-    bool live;
-    {
-        const int flat = row / a.split.group;
-        head = g.kv_head * a.split.group + (row - flat * a.split.group);
+    struct Row {
+        int b, token, head;
+        bool live;
+    };
+    auto row_of = [&](int lane) {
+        const int row = g.row0 + wr * 32 + (lane & 31);
+        const int flat = (int)((uint32_t)row / (uint32_t)a.split.group);
+        Row r{g.b, flat, g.kv_head * a.split.group + (row - flat * a.split.group), flat < g.count};
         if (g.b < 0) {
-            live = flat < cum_tokens[a.split.batch];
-            b = live ? find(cum_tokens, a.split.batch, flat) : 0;
-            token = live ? flat - cum_tokens[b] : 0;
-        } else {
-            live = flat < g.count;
-            token = flat;
+            r.live = flat < cum_tokens[a.split.batch];
+            r.b = r.live ? find(cum_tokens, a.split.batch, flat) : 0;
+            r.token = r.live ? flat - cum_tokens[r.b] : 0;
         }
-    }
+        return r;
+    };
+    const Row mine = row_of(lane);
+    const int own_limit = g.length + mine.token + 1;  // keys of its own that this row sees
+    const int own_first = own_common(a.split, g), own_last = own_end(a.split, g) - 1;
+
+    // Pages, 64 units ahead: lane l has the page of this wave's run of unit `paged` + l.
+    bool poison = g.bad;
+    uint32_t paged = g.first;
+    int pages;
+    auto look_up = [&]() {
+        const uint32_t u = smaller(paged + lane, g.end - 1);
+        const bool pre = u < g.prefix_units;
+        const int32_t* const table = pre ? a.prefix_table : a.block_table + (int64_t)max(g.b, 0) * a.split.max_pages;
+        const int first = run_start((int)(pre ? u : u - g.prefix_units) * kKeys, wave, pre ? a.prefix_len - 1 : own_last);
+        pages = (pre || !g.bad) ? table[first >> a.split.page_shift] : 0;
+        if ((uint32_t)pages >= (uint32_t)a.num_pages) {
+            pages = 0;
+            poison = true;
+        }
+    };
+    look_up();
+    const int64_t head_at = (int64_t)(g.kv_head << a.split.page_shift) * D;
+    struct Run {
+        int64_t at;  // of its first row, in the caches
+        int last;    // its last row; those behind repeat it
+    };
+    auto run_of = [&](uint32_t u) {
+        if (u - paged == 64) {
+            paged = u;
+            look_up();
+        }
+        const bool pre = u < g.prefix_units;
+        const int last = pre ? a.prefix_len - 1 : own_last;
+        const int first = run_start((int)(pre ? u : u - g.prefix_units) * kKeys, wave, last);
+        const int page = __builtin_amdgcn_readlane(pages, (int)(u - paged));
+        return Run{(int64_t)page * a.page_stride + head_at + (first & ((1 << a.split.page_shift) - 1)) * D, last - first};
+    };
+    // This wave's 16 rows of a unit of K (V), to its place in LDS.
+    auto stage = [&](const uint16_t* cache, const Run& run, uint32_t to) {
+        const int load_row = forget(lane) / S::kChunks, load_chunk = forget(lane) % S::kChunks;
+#pragma unroll
+        for (int j = 0; j < S::kLoads; ++j) {
+            const int in_run = j * S::kRowsLoad + load_row;
+            const int chunk = load_chunk ^ swizzle<D>(in_run);
+            const uint32_t offset = (uint32_t)(min(in_run, run.last) * D + chunk * 8) * 2;
+            if (D == S::kPitch || chunk * 8 < D)
+                load_to_lds(to + wave * (16 * S::kPitch * 2) + j * 1024, cache + run.at, offset);
+        }
+    };
+    Run run = run_of(g.first);
+    stage(a.k_cache, run, lds);
+    stage(a.v_cache, run, lds + S::kTile);
+
     V8 q[S::kSteps];
     {
-        const uint16_t* const from = a.q + b * a.q_stride[0] + token * a.q_stride[1] + head * a.q_stride[2] + half * 8;
+        const uint16_t* const from =
+            a.q + mine.b * a.q_stride[0] + mine.token * a.q_stride[1] + mine.head * a.q_stride[2] + half * 8;
 #pragma unroll
         for (int s = 0; s < S::kSteps; ++s) {
             u32x4 x = {0, 0, 0, 0};
-            if (live) x = *(const u32x4*)(from + 16 * s);
+            if (mine.live) x = *(const u32x4*)(from + 16 * s);
             q[s] = __builtin_bit_cast(V8, x);
         }
     }
-    const int own_limit = g.length + token + 1;                    // keys of its own that this row sees
-    const int own_first = own_common(a.split, g), own_last = own_end(a.split, g) - 1;
-
-    bool poison = g.bad;
-    f32x16 o[S::kOuts];
+    f32x16 o[kPieces];
 #pragma unroll
-    for (int i = 0; i < S::kOuts; ++i) o[i] = f32x16(0.0f);
+    for (int i = 0; i < kPieces; ++i) o[i] = f32x16(0.0f);
     float top = -INFINITY, sum = 0.0f;  // top: scores as they come from the product
-
-    // Loads of one unit: a wave stages 32 keys, in two runs of 16 that each lie in one page.
-    const uint16_t *run_k[2], *run_v[2];
-    int run_row[2];
-    auto turn = [&](uint32_t u) {  // to unit u: its pages
-        const bool pre = u < g.prefix_units;
-        const int base = (int)(pre ? u : u - g.prefix_units) * kKeys;
-        const int last = pre ? a.prefix_len - 1 : own_last;
-        const int32_t* const table = pre ? a.prefix_table : a.block_table + (int64_t)max(g.b, 0) * a.split.max_pages;
-        const int mask = (1 << a.split.page_shift) - 1;
-#pragma unroll
-        for (int r = 0; r < 2; ++r) {
-            const int first = run_start(base, wave * 2 + r, last);
-            int page = 0;
-            if (pre || !g.bad) page = table[first >> a.split.page_shift];
-            if ((uint32_t)page >= (uint32_t)a.num_pages) {
-                page = 0;
-                poison = true;
-            }
-            const int64_t at = (int64_t)page * a.page_stride + (int64_t)((g.kv_head << a.split.page_shift)) * D;
-            run_k[r] = a.k_cache + at + (int64_t)(first & mask) * D;
-            run_v[r] = a.v_cache + at + (int64_t)(first & mask) * D;
-            run_row[r] = last - first;  // rows of the run behind this one repeat it
-        }
-    };
-    const int load_row = lane / S::kChunks, load_chunk = lane % S::kChunks;
-    auto stage = [&](const uint16_t* const (&run)[2], uint32_t lds) {
-#pragma unroll
-        for (int j = 0; j < S::kLoads; ++j) {
-            constexpr int kRun = S::kLoads / 2;
-            const int r = j / kRun;
-            const int in_run = (j % kRun) * S::kRowsLoad + load_row;
-            const int chunk = load_chunk ^ swizzle<D>(r * 16 + in_run);
-            const uint32_t offset = (uint32_t)(min(in_run, run_row[r]) * D + chunk * 8) * 2;
-            if (D == S::kPitch || chunk * 8 < D) load_to_lds(lds + wave * (32 * S::kPitch * 2) + j * 1024, run[r], offset);
-        }
-    };
 
     // Places of this lane's reads.  The swizzle flips bits of the chunk's number
     // only, so a read's constant part comes by an exclusive or (chunk) or as an
@@ -346,104 +429,98 @@ __device__ void segment(const AttendArgs& a, const Segment& g, const int32_t* cu
     for (int j = 0; j < 2; ++j) {
         const int i = lane & 15, r = 8 * j + 4 * half + i / 4;
         const int chunk = ((lane >> 4) & 1) * 2 + (i % 4) / 2;
-        v_at[j] = S::kTile + block0 + r * (S::kPitch * 2) + ((chunk ^ swizzle<D>(r)) * 16) + (i & 1) * 8;
+        v_at[j] = block0 + r * (S::kPitch * 2) + (((chunk + 4 * wd) ^ swizzle<D>(r)) * 16) + (i & 1) * 8;
     }
-    // 8 values of V of the 16 keys from `key` on, in the order of the weights' registers
-    auto read_v = [&](int key, int out) {
-        i16x4 v[2];
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-            v[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                (SV_LDS i16x4*)(SV_LDS char*)(smem + (v_at[j] ^ (out * 64)) + key * (S::kPitch * 2)));
-        return __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7);
+
+    // Key 0 of unit u, the keys that this row sees of its sequence or prefix, and whether a row sees less than all.
+    auto base_of = [&](uint32_t u) { return (int)(u < g.prefix_units ? u : u - g.prefix_units) * kKeys; };
+    auto limit_of = [&](uint32_t u) { return u < g.prefix_units ? a.prefix_len : own_limit; };
+    auto partial_of = [&](uint32_t u) {
+        return base_of(u) + kKeys > (u < g.prefix_units ? a.prefix_len : own_first);
     };
-
-    turn(g.first);
-    stage(run_k, lds_k);
-    stage(run_v, lds_v);
-    for (uint32_t u = g.first; u < g.end; ++u) {
-        const bool pre = u < g.prefix_units;
-        const int base = (int)(pre ? u : u - g.prefix_units) * kKeys;
-        const int limit = pre ? a.prefix_len : own_limit;
-        const bool partial = base + kKeys > (pre ? a.prefix_len : own_first);
-        const bool more = u + 1 < g.end;
-
-        wait_loads<S::kLoads>();
-        lds_barrier();  // this unit's K is there
-        f32x16 p[NS];
-#pragma unroll
-        for (int s = 0; s < NS; ++s) p[s] = f32x16(0.0f);
-#pragma unroll
-        for (int c = 0; c < S::kSteps; ++c) {
-#pragma unroll
-            for (int s = 0; s < NS; ++s) {
-                const V8 k = *(const V8*)(smem + (k_at ^ (c * 32)) + s * (32 * S::kPitch * 2));
-                p[s] = T::mma(k, q[c], p[s]);
-            }
-        }
-        lds_barrier();  // every wave has read it
-        if (more) {
-            turn(u + 1);
-            stage(run_k, lds_k);
-        }
-
-        // scores to weights; key of register i: 8 (i / 4) + 4 half + i % 4
-        if (partial) {
+    auto k_read = [&](const char* tile, int m) {  // K's rows and columns of product m
+        return *(const V8*)(tile + (k_at ^ (m / NS * 32)) + m % NS * (32 * S::kPitch * 2));
+    };
+    // Masks unit u's scores, finds their maximum and moves the reference of the weights to it: they stay relative to
+    // a maximum of earlier units as long as the new one is within 2^8 of it, so nothing is rescaled for small rises.
+    auto refer = [&](uint32_t u, f32x16(&p)[NS], float most) {
+        if (partial_of(u)) {
+            const int key = base_of(u) + wk * NS * 32 + 4 * half, limit = limit_of(u);
+            most = -INFINITY;
 #pragma unroll
             for (int s = 0; s < NS; ++s)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int key = base + (wk * NS + s) * 32 + 8 * (i / 4) + 4 * half + (i % 4);
-                    p[s][i] = key < limit ? p[s][i] : -INFINITY;
+                for (int i = 0; i < 16; ++i) {  // key of register i: 8 (i / 4) + 4 half + i % 4
+                    p[s][i] = key + s * 32 + 8 * (i / 4) + i % 4 < limit ? p[s][i] : -INFINITY;
+                    most = fmaxf(most, p[s][i]);
                 }
         }
-        float most = -INFINITY;
-#pragma unroll
-        for (int s = 0; s < NS; ++s)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) most = fmaxf(most, p[s][i]);
         most = halves_max(most);
-        // Weights are relative to a maximum of earlier units as long as the new
-        // one is within 2^8 of it: nothing is rescaled for small rises.
         if (__any(most > top + a.lazy)) {
             const float now = fmaxf(top, most);
             const float by = (now == -INFINITY) ? 1.0f : exp2_hw((top - now) * a.scale_log2);
             sum *= by;
 #pragma unroll
-            for (int i = 0; i < S::kOuts; ++i) o[i] *= by;
+            for (int i = 0; i < kPieces; ++i) o[i] *= by;
             top = now;
         }
+    };
+    // One unit: p's scores are masked and referred to; `next` gets the scores of the unit after it.  The segment's
+    // even units lie in the first two tiles of LDS (K, V), its odd ones in the others.
+    auto step = [&](uint32_t u, auto odd, f32x16(&p)[NS], f32x16(&next)[NS]) {
+        constexpr int kHere = decltype(odd)::value * S::kStage, kThere = S::kStage - kHere;
+        const bool more = u + 1 < g.end;
+        char* const v_tile = smem + kHere + S::kTile;
         const float shift = (top == -INFINITY) ? 0.0f : -top * a.scale_log2;
         float add = 0.0f;
+        auto weigh = [&](int from, int to) {
 #pragma unroll
-        for (int s = 0; s < NS; ++s)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                p[s][i] = exp2_hw(fmaf(p[s][i], a.scale_log2, shift));
-                add += p[s][i];
+            for (int i = from; i < to; ++i) {
+                p[i / 16][i % 16] = exp2_hw(fmaf(p[i / 16][i % 16], a.scale_log2, shift));
+                add += p[i / 16][i % 16];
             }
+        };
+
+        stage_barrier();  // K of the next unit and V of this one are there, and every wave has done with those before
+        if (more) {
+            stage(a.v_cache, run, lds + kThere + S::kTile);
+            if (u + 2 < g.end) {
+                run = run_of(u + 2);
+                stage(a.k_cache, run, lds + kHere);
+            }
+            const char* const tile = smem + kThere;
+            V8 k[kAhead + 1];
+#pragma unroll
+            for (int m = 0; m < kAhead; ++m) k[m] = k_read(tile, m);
+#pragma unroll
+            for (int s = 0; s < NS; ++s) next[s] = f32x16(0.0f);
+#pragma unroll
+            for (int m = 0; m < kMmas; ++m) {
+                in_order();
+                if (m + kAhead < kMmas) k[(m + kAhead) % (kAhead + 1)] = k_read(tile, m + kAhead);
+                next[m % NS] = T::mma(k[m % (kAhead + 1)], q[m / NS], next[m % NS]);
+                weigh(m * NS * 16 / kMmas, (m + 1) * NS * 16 / kMmas);
+            }
+            in_order();
+        } else {
+            weigh(0, NS * 16);
+        }
         sum += add;
 
-        if (more)
-            wait_loads<S::kLoads>();
-        else
-            wait_loads<0>();
-        lds_barrier();  // this unit's V is there
-        if (partial && __syncthreads_or(special_chunks<T, D>(smem + S::kTile, false))) {
+        if (partial_of(u) && __syncthreads_or(special_chunks<T, D>(v_tile, false))) {
             // A masked key's weight is 0, but 0 times an infinity or NaN is not.
             // Rows take such values from the keys that they see, here; then they
             // are zeros for the product.
-            const int key0 = wk * NS * 32;
+            const int key0 = base_of(u) + wk * NS * 32, limit = limit_of(u), half = forget(lane) >> 5;
 #pragma unroll 1
             for (int k = 0; k < NS * 32; ++k) {
-                const bool sees = base + key0 + k < limit;
-                const int sw = swizzle<D>(k);
+                const bool sees = key0 + k < limit;
+                const char* const v_row = v_tile + block0 + k * (S::kPitch * 2) + half * 8;
 #pragma unroll
-                for (int i = 0; i < S::kOuts; ++i)
+                for (int i = 0; i < kPieces; ++i)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
-                        const u32x2 x = *(const u32x2*)(smem + S::kTile + (key0 + k) * (S::kPitch * 2) +
-                                                        ((4 * i + r) ^ sw) * 16 + half * 8);
+                        const u32x2 x = *(const u32x2*)(v_row + ((4 * (i * WD + wd) + r) ^ swizzle<D>(k)) * 16);
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
                             const uint32_t bits = (x[e / 2] >> (16 * (e % 2))) & 0xffffu;
@@ -452,131 +529,168 @@ __device__ void segment(const AttendArgs& a, const Segment& g, const int32_t* cu
                     }
             }
             __syncthreads();
-            special_chunks<T, D>(smem + S::kTile, true);
+            special_chunks<T, D>(v_tile, true);
             __syncthreads();
         }
+        // product m: 16 keys (m / kPieces) for one piece of the output
+        auto v_read = [&](int m) {
+            i16x4 x[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+                x[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((SV_LDS i16x4*)(SV_LDS char*)(
+                    v_tile + (v_at[j] ^ (m % kPieces * WD * 64)) + m / kPieces * (16 * S::kPitch * 2)));
+            return __builtin_bit_cast(V8, __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7));
+        };
+        V8 v[kAheadV + 1], w8;
+#pragma unroll
+        for (int m = 0; m < kAheadV; ++m) v[m] = v_read(m);
+        float most = -INFINITY;
+#pragma unroll
+        for (int m = 0; m < kMmasV; ++m) {
+            const int block = m / kPieces;
+            if (m % kPieces == 0) {
+                f32x8 w;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) w[i] = p[block / 2][8 * (block % 2) + i];
+                w8 = __builtin_convertvector(w, V8);
+            }
+            in_order();
+            if (m + kAheadV < kMmasV) v[(m + kAheadV) % (kAheadV + 1)] = v_read(m + kAheadV);
+            o[m % kPieces] = T::mma(v[m % (kAheadV + 1)], w8, o[m % kPieces]);
+#pragma unroll
+            for (int i = m * NS * 16 / kMmasV; i < (m + 1) * NS * 16 / kMmasV; ++i) most = fmaxf(most, next[i / 16][i % 16]);
+        }
+        in_order();
+        if (more) refer(u + 1, next, most);
+    };
+
+    f32x16 scores[2][NS];
+    {
+        stage_barrier();  // the first unit's K
+        if (g.first + 1 < g.end) {
+            run = run_of(g.first + 1);
+            stage(a.k_cache, run, lds + S::kStage);
+        }
+        float most = -INFINITY;
+#pragma unroll
+        for (int s = 0; s < NS; ++s) scores[0][s] = scores[1][s] = f32x16(0.0f);
+#pragma unroll
+        for (int m = 0; m < kMmas; ++m) scores[0][m % NS] = T::mma(k_read(smem, m), q[m / NS], scores[0][m % NS]);
 #pragma unroll
         for (int s = 0; s < NS; ++s)
 #pragma unroll
-            for (int kb = 0; kb < 2; ++kb) {
-                f32x8 w;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) w[i] = p[s][8 * kb + i];
-                const V8 w8 = __builtin_convertvector(w, V8);
-#pragma unroll
-                for (int i = 0; i < S::kOuts; ++i)
-                    o[i] = T::mma(__builtin_bit_cast(V8, read_v(s * 32 + kb * 16, i)), w8, o[i]);
-            }
-        lds_barrier();  // every wave has read V
-        if (more) stage(run_v, lds_v);
+            for (int i = 0; i < 16; ++i) most = fmaxf(most, scores[0][s][i]);
+        refer(g.first, scores[0], most);
+    }
+    for (uint32_t u = g.first; u < g.end; u += 2) {
+        step(u, std::integral_constant<int, 0>(), scores[0], scores[1]);
+        if (u + 1 < g.end) step(u + 1, std::integral_constant<int, 1>(), scores[1], scores[0]);
     }
 
     // ---- join the waves that split the keys, then write
-    sum = halves_sum(sum);
-    top *= a.scale_log2;
-    if (poison) *poison_flag = 1;
-    if constexpr (WK > 1) {
-        float(*const mine)[32] = wave_stats[wave];
-        if (half == 0) {
-            mine[0][lane] = top;
-            mine[1][lane] = sum;
-        }
-        __syncthreads();
-        float now = -INFINITY;
-#pragma unroll
-        for (int k = 0; k < WK; ++k) now = fmaxf(now, wave_stats[wr + k * WR][0][lane & 31]);
-        const float ref = (now == -INFINITY) ? 0.0f : now;
-        float all = 0.0f;
-#pragma unroll
-        for (int k = 0; k < WK; ++k)
-            all += wave_stats[wr + k * WR][1][lane & 31] * exp2_hw(wave_stats[wr + k * WR][0][lane & 31] - ref);
-        const float by = exp2_hw(top - ref);
-        // piece i of the output is summed by the wave wk = i % WK
-        f32x4* const box = (f32x4*)smem;  // [from][row block][piece][4][lane]
-#pragma unroll
-        for (int i = 0; i < S::kOuts; ++i) {
-            o[i] *= by;
-            if (i % WK != wk) {
-                const int from = wk < i % WK ? wk : wk - 1;
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const f32x4 x = {o[i][4 * r], o[i][4 * r + 1], o[i][4 * r + 2], o[i][4 * r + 3]};
-                    box[(((from * WR + wr) * S::kOuts + i) * 4 + r) * 64 + lane] = x;
-                }
+    auto finish = [&](int lane) {
+        const int half = lane >> 5;
+        if constexpr (WK > 1) {
+            if (half == 0) {
+                wave_stats[wave][0][lane] = top;
+                wave_stats[wave][1][lane] = sum;
             }
-        }
-        __syncthreads();
+            lds_barrier();
+            const float(*const other)[32] = wave_stats[wave + (wk == 0 ? WR : -WR)];
+            const float other_top = other[0][lane & 31], now = fmaxf(top, other_top);
+            const float ref = (now == -INFINITY) ? 0.0f : now;
+            const float by = exp2_hw(top - ref);
+            const float own = by * sum, others = exp2_hw(other_top - ref) * other[1][lane & 31];
+            sum = wk == 0 ? own + others : others + own;
+            top = now;
+            // piece i of the output is summed by the wave wk = i % WK
+            f32x4* const box = (f32x4*)smem;  // [row block, head_dim part][piece][4][lane]
+            const int pair = wr + wd * WR;
 #pragma unroll
-        for (int i = 0; i < S::kOuts; ++i) {
-            if (i % WK == wk) {
-#pragma unroll
-                for (int from = 0; from < WK - 1; ++from)
+            for (int i = 0; i < kPieces; ++i) {
+                o[i] *= by;
+                if (i % WK != wk) {
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
-                        const f32x4 x = box[(((from * WR + wr) * S::kOuts + i) * 4 + r) * 64 + lane];
+                        const f32x4 x = {o[i][4 * r], o[i][4 * r + 1], o[i][4 * r + 2], o[i][4 * r + 3]};
+                        box[((pair * kPieces + i) * 4 + r) * 64 + lane] = x;
+                    }
+                }
+            }
+            lds_barrier();
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) {
+                if (i % WK == wk) {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const f32x4 x = box[((pair * kPieces + i) * 4 + r) * 64 + lane];
 #pragma unroll
                         for (int e = 0; e < 4; ++e) o[i][4 * r + e] += x[e];
                     }
-            }
-        }
-        top = now;
-        sum = all;
-    } else {
-        __syncthreads();
-    }
-    const bool nan = *poison_flag != 0;
-    if (whole) {
-        const float by = nan ? NAN : 1.0f / sum;
-        uint16_t* const to = a.out + b * a.out_stride[0] + token * a.out_stride[1] + head * a.out_stride[2];
-#pragma unroll
-        for (int i = 0; i < S::kOuts; ++i)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int d = 32 * i + 8 * r + 4 * half;
-                if (live && i % WK == wk && d < D) {
-                    f32x4 x = {o[i][4 * r], o[i][4 * r + 1], o[i][4 * r + 2], o[i][4 * r + 3]};
-                    x *= by;
-                    *(u32x2*)(to + d) = __builtin_bit_cast(u32x2, __builtin_convertvector(x, typename T::V4));
                 }
             }
-    } else {
-        const int64_t at = place + wr * 32 + (lane & 31);
-        if (half == 0 && wk == 0) {
-            a.part_max[at] = top;
-            a.part_sum[at] = sum;
         }
-        float* const to = a.part_out + at * D;
+        const bool nan = *poison_flag != 0;
+        const float by = nan ? NAN : whole ? 1.0f / sum : 1.0f;
+        if (!whole && half == 0 && wk == 0 && wd == 0) {
+            a.part_max[place + wr * 32 + lane] = top;
+            a.part_sum[place + wr * 32 + lane] = sum;
+        }
+        // A lane has 16 values of its row; they go out by way of LDS, 8 lanes a row, in
+        // whole lines of 128 bytes.
+        f32x4* const turn = (f32x4*)(smem + 2 * S::kTile + wave * 4096);  // (behind the box) [row][8], chunks flipped by row
 #pragma unroll
-        for (int i = 0; i < S::kOuts; ++i)
+        for (int i = 0; i < kPieces; ++i) {
+            if (i % WK != wk) continue;
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const int d = 32 * i + 8 * r + 4 * half;
-                if (i % WK == wk && d < D) {
-                    f32x4 x = {o[i][4 * r], o[i][4 * r + 1], o[i][4 * r + 2], o[i][4 * r + 3]};
-                    if (nan) x = f32x4(NAN);
-                    *(f32x4*)(to + d) = x;
+                const f32x4 x = {o[i][4 * r], o[i][4 * r + 1], o[i][4 * r + 2], o[i][4 * r + 3]};
+                turn[(lane & 31) * 8 + ((2 * r + half) ^ (lane & 7))] = x * by;
+            }
+            __builtin_amdgcn_wave_barrier();
+            const int d = 32 * (i * WD + wd) + 4 * (lane & 7);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int row = 8 * j + lane / 8;
+                const f32x4 x = turn[row * 8 + ((lane & 7) ^ (row & 7))];
+                if (d >= D) continue;
+                if (whole) {
+                    const Row to = row_of(row);
+                    if (to.live)
+                        *(u32x2*)(a.out + to.b * a.out_stride[0] + to.token * a.out_stride[1] + to.head * a.out_stride[2] + d) =
+                            __builtin_bit_cast(u32x2, __builtin_convertvector(x, typename T::V4));
+                } else {
+                    *(f32x4*)(a.part_out + (place + wr * 32 + row) * D + d) = x;
                 }
             }
-    }
-    __syncthreads();  // LDS and the flag are free again
+            __builtin_amdgcn_wave_barrier();
+        }
+    };
+    sum = halves_sum(sum);
+    top *= a.scale_log2;
+    if (poison) *poison_flag = 1;
+    lds_barrier();  // every wave has done with the tiles
+    finish(forget(lane));
+    lds_barrier();  // LDS and the flag are free again
     if (tid == 0) *poison_flag = 0;
 }
 
-template <class T, int D>
+// kPrefix and kOwn: waves that split the rows of the prefix's tasks and of the sequences' own.
+template <class T, int D, int kPrefix, int kOwn>
 __global__ void __launch_bounds__(kThreads, (D > 128 ? 1 : 2)) attend_kernel(AttendArgs a) {
     extern __shared__ __attribute__((aligned(16))) char smem[];
     __shared__ uint32_t wave_sums[4][2];
     __shared__ float wave_stats[4][2][32];
     __shared__ int poison_flag;
     const Split& split = a.split;
-    int32_t* const cum_tokens = (int32_t*)(smem + 2 * Shape<D>::kTile);
-    uint32_t* const cum_units = (uint32_t*)(cum_tokens + split.batch + 1);
+    int32_t* const words = (int32_t*)(smem + 2 * Shape<D>::kStage);
+    const Batch batch{words, (uint32_t*)words + split.batch + 1, words + 2 * (split.batch + 1)};
     if (threadIdx.x == 0) poison_flag = 0;
-    const Totals t = sum_batch(split, cum_tokens, cum_units, wave_sums);
+    const Totals t = sum_batch(split, batch, wave_sums);
     if (blockIdx.x == 0)  // for the kernel that joins the parts
         for (int b = threadIdx.x; b <= split.batch; b += kThreads) {
-            a.cum_tokens[b] = cum_tokens[b];
-            a.cum_units[b] = cum_units[b];
+            a.cum_tokens[b] = batch.cum_tokens[b];
+            a.cum_cost[b] = batch.cum_cost[b];
         }
     if (blockIdx.x >= t.groups) return;
     // Workgroups go round the 8 XCDs; those of one XCD take adjoining runs, so
@@ -584,19 +698,18 @@ __global__ void __launch_bounds__(kThreads, (D > 128 ? 1 : 2)) attend_kernel(Att
     const uint32_t w = (t.groups % 8 == 0) ? (blockIdx.x % 8) * (t.groups / 8) + blockIdx.x / 8 : blockIdx.x;
     const uint32_t end = group_start(t, w + 1);
     for (uint32_t u = group_start(t, w); u < end;) {
-        Segment g = task_at(split, t, cum_units, u);
-        g.first = u - g.task_start;
-        g.end = smaller(g.units, end - g.task_start);
+        Segment g = task_at(split, t, batch.cum_cost, u, [&](int32_t b) { return sequence(batch, b); });
+        cut(g, u, end);
+        if (g.first == g.end) break;  // (the run ends within the task's cost of starting)
         const bool whole = whole_task(split, g);
         const int64_t place = part_place(split, g, w);
-        const int waves = (g.b < 0 ? split.plan.prefix_rows : split.plan.own_rows) / 32;
-        if (waves == 1)
-            segment<T, D, 1>(a, g, cum_tokens, smem, wave_stats, &poison_flag, whole, place);
-        else if (waves == 2 || D > 128)
-            segment<T, D, 2>(a, g, cum_tokens, smem, wave_stats, &poison_flag, whole, place);
-        else if constexpr (D <= 128)
-            segment<T, D, 4>(a, g, cum_tokens, smem, wave_stats, &poison_flag, whole, place);
         u = g.task_start + g.end;
+        g.first += g.offset;  // (from here on: units of the keys)
+        g.end += g.offset;
+        if (kPrefix == kOwn || g.b >= 0)
+            segment<T, D, kOwn>(a, g, batch.cum_tokens, smem, wave_stats, &poison_flag, whole, place);
+        else
+            segment<T, D, kPrefix>(a, g, batch.cum_tokens, smem, wave_stats, &poison_flag, whole, place);
     }
 }
 
@@ -604,77 +717,144 @@ __global__ void __launch_bounds__(kThreads, (D > 128 ? 1 : 2)) attend_kernel(Att
 // joining the parts
 // ---------------------------------------------------------------------------
 
-template <class T, int D>
-__device__ __forceinline__ void join(const AttendArgs& a, const Parts (&parts)[2], int d, uint16_t* to) {
-    float top = -INFINITY;
-    for (int l = 0; l < 2; ++l)
-        for (int k = 0; k < parts[l].n; ++k) top = fmaxf(top, a.part_max[parts[l].first + k * parts[l].step]);
+// One row of the output from its parts, by one wave; `place(k)` is the row place
+// of part k of n, or -1.  Bound by the latency of its dependent loads: first the
+// parts' statistics, a part a lane, then their outputs, D / 4 lanes a part, as many
+// parts side by side as fit the wave and four such rounds under way at a time.
+template <class T, int D, class Place>
+__device__ __forceinline__ void join(const AttendArgs& a, int n, Place place, uint16_t* to) {
+    constexpr int kLanes = D / 4, kTeams = 64 / kLanes, kAhead = 4;
+    const int lane = threadIdx.x & 63;
+    const int team = min(lane / kLanes, kTeams - 1), d = (lane % kLanes) * 4;
+    float top = -INFINITY, sum = 0.0f;
     f32x4 out = f32x4(0.0f);
-    float sum = 0.0f;
-    for (int l = 0; l < 2; ++l)
-        for (int k = 0; k < parts[l].n; ++k) {
-            const int64_t at = parts[l].first + k * parts[l].step;
-            const float by = exp2_hw(a.part_max[at] - top);
-            sum += by * a.part_sum[at];
-            out += by * *(const f32x4*)(a.part_out + at * D + d);
+    for (int base = 0; base < n; base += 64) {
+        int64_t at = (base + lane < n) ? place(base + lane) : -1;
+        // the parts that there are, to the first lanes
+        const uint64_t there = __ballot(at >= 0);
+        const int count = __popcll(there);
+        if (count == 0) continue;
+        if (count < 64) {
+            const int slot = at >= 0 ? __popcll(there & ((1ull << lane) - 1)) : 63;  // (63 is no part's here)
+            const int low = __builtin_amdgcn_ds_permute(slot * 4, (int)(uint32_t)at);
+            const int high = __builtin_amdgcn_ds_permute(slot * 4, (int)(at >> 32));
+            at = ((int64_t)high << 32) | (uint32_t)low;
         }
-    out *= 1.0f / sum;
-    *(u32x2*)(to + d) = __builtin_bit_cast(u32x2, __builtin_convertvector(out, typename T::V4));
+        const float most = lane < count ? a.part_max[at] : -INFINITY;
+        const float part_sum = lane < count ? a.part_sum[at] : 0.0f;
+        float now = fmaxf(top, most);
+#pragma unroll
+        for (int m = 1; m < 64; m <<= 1) now = fmaxf(now, __shfl_xor(now, m));
+        const float ref = now == -INFINITY ? 0.0f : now;
+        const float before = exp2_hw(top - ref), by = lane < count ? exp2_hw(most - ref) : 0.0f;
+        sum = before * sum + by * part_sum;
+        out *= before;
+        top = now;
+        for (int k0 = 0; k0 < count; k0 += kAhead * kTeams) {
+            f32x4 x[kAhead];
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j) {
+                const int k = min(k0 + j * kTeams + team, count - 1);
+                const int64_t from = ((int64_t)__shfl((int)(at >> 32), k) << 32) | (uint32_t)__shfl((int)(uint32_t)at, k);
+                x[j] = *(const f32x4*)(a.part_out + from * D + d);
+            }
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j) {
+                const int k = k0 + j * kTeams + team;
+                const float w = __shfl(by, min(k, count - 1));
+                if (k < count) out += w * x[j];
+            }
+        }
+    }
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) sum += __shfl_xor(sum, m);
+    f32x4 all = out;
+#pragma unroll
+    for (int t = 1; t < kTeams; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) all[e] += __shfl(out[e], (lane + t * kLanes) & 63);
+    if (lane >= kLanes) return;
+    all *= 1.0f / sum;
+    *(u32x2*)(to + d) = __builtin_bit_cast(u32x2, __builtin_convertvector(all, typename T::V4));
 }
 
-// Rows of a batch with a shared prefix: every row has parts of both.
+// Rows of a batch with a shared prefix: every row has parts of both.  A wave a row.
 template <class T, int D>
 __global__ void __launch_bounds__(kThreads) attend_join_rows_kernel(AttendArgs a) {
-    constexpr int kLanes = D / 4, kRowsBlock = kThreads / kLanes;
     const Split& split = a.split;
-    const int lane = threadIdx.x % kLanes;
-    const int64_t row = (int64_t)blockIdx.x * kRowsBlock + threadIdx.x / kLanes;
-    if (threadIdx.x >= kRowsBlock * kLanes || row >= (int64_t)split.batch * split.max_new * a.q_heads) return;
-    const int head = (int)(row % a.q_heads);
-    const int64_t flat = row / a.q_heads;
-    const int token = (int)(flat % split.max_new), b = (int)(flat / split.max_new);
+    const int64_t row = (int64_t)blockIdx.x * (kThreads / 64) + uniform((int32_t)(threadIdx.x >> 6));
+    if (row >= (int64_t)split.batch * split.max_new * a.q_heads) return;
+    const int head = (int)((uint32_t)row % (uint32_t)a.q_heads);
+    const uint32_t flat = (uint32_t)row / (uint32_t)a.q_heads;
+    const int token = (int)(flat % (uint32_t)split.max_new), b = (int)(flat / (uint32_t)split.max_new);
     const Sequence s = sequence(split, b);
     if (token >= s.count) return;
-    const Totals t = totals(split, a.cum_tokens[split.batch], a.cum_units[split.batch]);
+    const Totals t = totals(split, a.cum_tokens[split.batch], a.cum_cost[split.batch]);
     const int kv_head = head / split.group, g = head - kv_head * split.group;
-    const Parts parts[2] = {prefix_parts(split, t, a.cum_tokens[b], token, kv_head, g),
-                            own_parts(split, t, s, a.cum_units[b], a.cum_units[b + 1] - a.cum_units[b], b, token,
-                                      kv_head, g)};
-    join<T, D>(a, parts, lane * 4, a.out + b * a.out_stride[0] + token * a.out_stride[1] + head * a.out_stride[2]);
+    const Parts own =
+        own_parts(split, t, s, a.cum_cost[b], a.cum_cost[b + 1] - a.cum_cost[b], b, token, kv_head, g);
+    const int prefix = (int)(kChunkParts * t.chunks), r = (a.cum_tokens[b] + token) * split.group + g;
+    join<T, D>(a, prefix + own.n,
+               [&](int k) {
+                   return k < prefix ? prefix_part(split, t, kv_head, r, (uint32_t)k) : own.first + (k - prefix) * own.step;
+               },
+               a.out + b * a.out_stride[0] + token * a.out_stride[1] + head * a.out_stride[2]);
 }
 
 // Tasks that the workgroups' borders cut: block x looks at the border before
-// workgroup x + 1, and joins the task that it cuts if it is the first to.
+// workgroup x + 1, and joins the task that it cuts if it is the first to; block y
+// takes kJoinRows of its rows.
+constexpr int kJoinRows = 16;
 template <class T, int D>
 __global__ void __launch_bounds__(kThreads) attend_join_tasks_kernel(AttendArgs a) {
     const Split& split = a.split;
-    const Totals t = totals(split, uniform(a.cum_tokens[split.batch]), uniform(a.cum_units[split.batch]));
+    const Totals t = totals(split, uniform(a.cum_tokens[split.batch]), uniform(a.cum_cost[split.batch]));
     const uint32_t w = blockIdx.x + 1;
     if (w >= t.groups) return;
-    const uint32_t u = group_start(t, w);
-    const Segment g = task_at(split, t, a.cum_units, u);
-    const uint32_t w0 = group_of(t, g.task_start), w1 = group_of(t, g.task_start + g.units - 1);
-    if (u == g.task_start || w != w0 + 1) return;
-    constexpr int kLanes = D / 4;
-    for (int at = threadIdx.x; at < split.plan.own_rows * kLanes; at += kThreads) {
-        const int r = at / kLanes, d = (at - r * kLanes) * 4, row = g.row0 + r;
+    const Segment g =
+        task_at(split, t, a.cum_cost, group_start(t, w), [&](int32_t b) { return sequence(split, b); });
+    uint32_t w0, w1;
+    if (!first_border(t, g, w, w0, w1)) return;
+    const int wave = uniform((int32_t)(threadIdx.x >> 6));
+#pragma unroll 1
+    for (int i = wave; i < kJoinRows; i += kThreads / 64) {
+        const int r = (int)blockIdx.y * kJoinRows + i, row = g.row0 + r;
         const int token = row / split.group, head = g.kv_head * split.group + (row - token * split.group);
-        if (token >= g.count) continue;
-        const Parts parts[2] = {first_cut_part(split, w0, r), later_cut_parts(split, w0, w1, r)};
-        join<T, D>(a, parts, d, a.out + g.b * a.out_stride[0] + token * a.out_stride[1] + head * a.out_stride[2]);
+        if (token >= g.count) return;
+        const Parts first = first_cut_part(split, w0, r), later = later_cut_parts(split, w0, w1, r);
+        join<T, D>(a, 1 + later.n, [&](int k) { return k == 0 ? first.first : later.first + (k - 1) * later.step; },
+                   a.out + g.b * a.out_stride[0] + token * a.out_stride[1] + head * a.out_stride[2]);
     }
 }
 
+// (at head_dim 256 a task has at most 64 rows, see task_rows)
+template <int D>
+constexpr int kMaxTaskRows = D > 128 ? 64 : 128;
+
 template <class T, int D>
 sv_status_t launch(const AttendArgs& a, hipStream_t stream) {
-    const size_t lds = 2 * Shape<D>::kTile + 2 * sizeof(int32_t) * ((size_t)a.split.batch + 1);
+    const size_t lds = 2 * Shape<D>::kStage + 3 * sizeof(int32_t) * ((size_t)a.split.batch + 1);
     const uint32_t groups = (uint32_t)a.split.plan.groups;
-    hipLaunchKernelGGL((attend_kernel<T, D>), dim3(groups), dim3(kThreads), lds, stream, a);
+    const int own = a.split.plan.own_rows / 32, prefix = a.split.plan.joined ? own : a.split.plan.prefix_rows / 32;
+    auto go = [&](auto p, auto o) {
+        hipLaunchKernelGGL((attend_kernel<T, D, decltype(p)::value, decltype(o)::value>), dim3(groups), dim3(kThreads),
+                           lds, stream, a);
+    };
+    constexpr std::integral_constant<int, 1> k1{};
+    constexpr std::integral_constant<int, 2> k2{};
+    constexpr std::integral_constant<int, kMaxTaskRows<D> / 32> k4{};
+    if (prefix == 1)
+        go(k1, k1);
+    else if (prefix == 2)
+        own == 1 ? go(k2, k1) : go(k2, k2);
+    else
+        own == 1 ? go(k4, k1) : own == 2 ? go(k4, k2) : go(k4, k4);
     if (a.split.plan.joined) {
         if (groups > 1)
-            hipLaunchKernelGGL((attend_join_tasks_kernel<T, D>), dim3(groups - 1), dim3(kThreads), 0, stream, a);
+            hipLaunchKernelGGL((attend_join_tasks_kernel<T, D>), dim3(groups - 1, a.split.plan.own_rows / kJoinRows),
+                               dim3(kThreads), 0, stream, a);
     } else {
-        constexpr int kRowsBlock = kThreads / (D / 4);
+        constexpr int kRowsBlock = kThreads / 64;
         const int64_t rows = (int64_t)a.split.batch * a.split.max_new * a.q_heads;
         hipLaunchKernelGGL((attend_join_rows_kernel<T, D>), dim3((uint32_t)((rows + kRowsBlock - 1) / kRowsBlock)),
                            dim3(kThreads), 0, stream, a);
@@ -730,7 +910,7 @@ sv_status_t spec_cache_attend(const sv_cache_attend_desc_t* desc, hipStream_t st
     a.lazy = 8.0f / a.scale_log2;
     char* ws = static_cast<char*>(d.workspace);
     a.cum_tokens = reinterpret_cast<int32_t*>(ws);
-    a.cum_units = reinterpret_cast<uint32_t*>(ws + plan.cum_bytes);
+    a.cum_cost = reinterpret_cast<uint32_t*>(ws + plan.cum_bytes);
     a.part_max = reinterpret_cast<float*>(ws + 2 * plan.cum_bytes);
     a.part_sum = a.part_max + plan.rows;
     a.part_out = a.part_sum + plan.rows;

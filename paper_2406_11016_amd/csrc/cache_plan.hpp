@@ -51,8 +51,13 @@ inline sv_status_t check_cache(sv_dtype_t dtype, int32_t batch, int32_t max_new,
 // attention
 // ---------------------------------------------------------------------------
 
-// Keys of a unit of work: what a workgroup holds of K and V at a time.
-constexpr int kAttendKeys = 128;
+// Keys of a unit of work: what a workgroup holds of K and V twice, the unit it
+// computes and the one on its way.
+constexpr int kAttendKeys = 64;
+
+// What a workgroup's start and end with a task cost it, in units: tasks count that
+// many units more where work is dealt out.
+constexpr uint32_t kTaskUnits = 3;
 
 // How a call's work is cut (see cache_attend.hip).
 struct AttendPlan {
@@ -62,6 +67,7 @@ struct AttendPlan {
     bool joined;
     int32_t own_rows, own_tiles;  // rows of a sequence's own task (32, 64 or 128); tasks a key/value head
     int32_t prefix_rows;          // rows of a prefix task
+    int32_t own_shift, prefix_shift;  // their logarithms
     int32_t groups;               // workgroups
     int64_t own_parts, rows;      // row places of the parts: of the first own one, of all
     size_t cum_bytes;             // one array of sums over the batch
@@ -88,13 +94,16 @@ inline AttendPlan attend_plan(int32_t batch, int32_t max_new, int32_t q_heads, i
     p.own_rows = task_rows(rows, head_dim);
     p.own_tiles = (int32_t)((rows + p.own_rows - 1) / p.own_rows);
     p.prefix_rows = task_rows(batch * rows, head_dim);
+    p.own_shift = __builtin_ctz((unsigned)p.own_rows);
+    p.prefix_shift = __builtin_ctz((unsigned)p.prefix_rows);
     p.groups = head_dim > 128 ? 256 : 512;  // what the 256 CUs hold at a time: one of 128 KiB LDS each, or two of 64
     if (p.joined) {
         p.own_parts = 0;
         p.rows = 2 * (int64_t)p.groups * p.own_rows;
     } else {
         const int64_t prefix_tasks = kv_heads * ((batch * rows + p.prefix_rows - 1) / p.prefix_rows);
-        p.own_parts = (prefix_tasks + p.groups) * p.prefix_rows;
+        // (chunks of the prefix are at least half a workgroup's share, see Totals: at most 2 * groups tasks more)
+        p.own_parts = (prefix_tasks + 3 * p.groups + 1) * p.prefix_rows;
         p.rows = p.own_parts + ((int64_t)batch * kv_heads * p.own_tiles + p.groups) * p.own_rows;
     }
     p.cum_bytes = (sizeof(int32_t) * ((size_t)batch + 1) + 255) / 256 * 256;
@@ -107,14 +116,15 @@ inline bool attend_sizes_ok(int32_t batch, int32_t max_new, int32_t q_heads, int
            (int64_t)batch * max_new <= INT_MAX && (int64_t)batch * max_new * q_heads <= INT_MAX;
 }
 
-// The numbers of units fit 31 bits at the longest sequences that the table can name.
+// The numbers of units (with what the tasks cost) fit 31 bits at the longest sequences that the table can name.
 inline bool attend_units_ok(const sv_cache_attend_desc_t& d, const AttendPlan& p) {
     const int64_t pre = ((int64_t)d.prefix_len + kAttendKeys - 1) / kAttendKeys;
     const int64_t own = ((int64_t)d.max_pages * d.page_size + kAttendKeys - 1) / kAttendKeys;
     const double tiles = (double)d.batch * d.kv_heads * p.own_tiles;
     const double rows = (double)d.batch * d.max_new * (d.q_heads / d.kv_heads);
-    const double pooled = p.joined ? 0.0 : d.kv_heads * (double)pre * (rows / p.prefix_rows + 1.0);
-    return tiles * (double)(own + (p.joined ? pre : 0)) + pooled < 2147483647.0;
+    // (a chunk of the prefix has a unit at least)
+    const double pooled = p.joined ? 0.0 : d.kv_heads * (double)pre * (1 + kTaskUnits) * (rows / p.prefix_rows + 1.0);
+    return tiles * (double)(own + kTaskUnits + (p.joined ? pre : 0)) + pooled < 2147483647.0;
 }
 
 inline size_t attend_workspace_bytes(int32_t batch, int32_t max_new, int32_t q_heads, int32_t kv_heads,

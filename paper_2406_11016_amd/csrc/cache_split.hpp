@@ -55,40 +55,60 @@ constexpr Sequence sequence(const Split& a, int32_t b) {
 
 // Units of row tile rt of a sequence's own tasks (of each key/value head).
 constexpr uint32_t tile_units(const Split& a, const Sequence& s, int32_t rt) {
-    const int32_t first = rt * a.plan.own_rows;
+    const int32_t first = rt << a.plan.own_shift;
     if (first >= s.count * a.group) return 0;
-    const int32_t last = smaller(s.count - 1, (first + a.plan.own_rows - 1) / a.group);
+    const int32_t last =
+        smaller(s.count - 1, (int32_t)((uint32_t)(first + a.plan.own_rows - 1) / (uint32_t)a.group));
     const uint32_t own = ((uint32_t)s.length + (uint32_t)last + kAttendKeys) / kAttendKeys;
     return own + (a.plan.joined ? (uint32_t)a.prefix_units : 0u);
 }
-constexpr uint32_t sequence_units(const Split& a, const Sequence& s) {
-    uint32_t n = 0;
-    for (int32_t rt = 0; rt < a.plan.own_tiles; ++rt) n += tile_units(a, s, rt);
-    return n;
+constexpr uint32_t tile_cost(const Split& a, const Sequence& s, int32_t rt) {
+    const uint32_t n = tile_units(a, s, rt);
+    return n == 0 ? 0 : n + kTaskUnits;
 }
 
-// The tasks in order: the shared prefix's (key/value head, then row tile), then
-// each sequence's own (sequence, head, row tile).
+// The tasks in order: the shared prefix's, then each sequence's own (sequence, head,
+// row tile).  The prefix is cut into chunks of a workgroup's share of all units,
+// and its tasks are ordered by key/value head, chunk, row tile: workgroups next to
+// each other then run over the same keys at the same time, for other rows, and
+// find them in their XCD's L2.  (With tasks over the whole prefix every workgroup
+// was somewhere else in it: 18,432 rows and 16,384 keys read 1.07 GB from behind
+// the L2s at 5.8 TB/s, which took 183 us, whatever was computed.)
 struct Totals {
     int32_t tokens, prefix_tiles;  // prefix tiles of one key/value head
-    uint32_t prefix_units, units;  // units of all prefix tasks; of all tasks
-    uint32_t groups;               // workgroups that take part: each has a unit
+    uint32_t prefix_cost, cost;    // cost of all prefix tasks; of all tasks
+    uint32_t groups;               // workgroups that take part
+    uint32_t each, longer;         // cost dealt to a workgroup; the first `longer` have one more
+    uint32_t chunk, chunks;        // units of a chunk of the prefix; chunks
 };
-constexpr Totals totals(const Split& a, int32_t tokens, uint32_t own_units) {
+constexpr Totals totals(const Split& a, int32_t tokens, uint32_t own_cost) {
     Totals t{};
     t.tokens = tokens;
-    t.prefix_tiles =
-        a.plan.joined ? 0 : (int32_t)(((int64_t)tokens * a.group + a.plan.prefix_rows - 1) / a.plan.prefix_rows);
-    t.prefix_units = (uint32_t)t.prefix_tiles * (uint32_t)a.prefix_units * (uint32_t)a.kv_heads;
-    t.units = t.prefix_units + own_units;
-    t.groups = smaller((uint32_t)a.plan.groups, t.units);
+    if (!a.plan.joined)
+        t.prefix_tiles =
+            (int32_t)(((uint32_t)tokens * (uint32_t)a.group + (uint32_t)a.plan.prefix_rows - 1) >> a.plan.prefix_shift);
+    const uint32_t rows_heads = (uint32_t)t.prefix_tiles * (uint32_t)a.kv_heads, units = (uint32_t)a.prefix_units;
+    t.cost = rows_heads * (units + kTaskUnits) + own_cost;
+    t.groups = smaller((uint32_t)a.plan.groups, t.cost);
+    if (t.groups == 0) return t;
+    if (rows_heads != 0) {
+        const uint32_t share = t.cost / t.groups;
+        t.chunk = share > 2 * kTaskUnits ? share - kTaskUnits : 1 + share / 2;
+        t.chunks = (units + t.chunk - 1) / t.chunk;
+        t.prefix_cost = rows_heads * (units + t.chunks * kTaskUnits);
+        t.cost = t.prefix_cost + own_cost;
+        t.groups = smaller((uint32_t)a.plan.groups, t.cost);
+    }
+    t.each = t.cost / t.groups;
+    t.longer = t.cost - t.each * t.groups;
     return t;
 }
 
-// Workgroup w's run of units begins at group_start(w); group_of is its inverse.
-constexpr uint32_t group_start(const Totals& t, uint32_t w) { return (uint32_t)((uint64_t)w * t.units / t.groups); }
+// Workgroup w's run of the cost begins at group_start(w); group_of is its inverse.
+constexpr uint32_t group_start(const Totals& t, uint32_t w) { return w * t.each + smaller(w, t.longer); }
 constexpr uint32_t group_of(const Totals& t, uint32_t u) {
-    return (uint32_t)((((uint64_t)u + 1) * t.groups - 1) / t.units);
+    const uint32_t border = t.longer * (t.each + 1);
+    return u < border ? u / (t.each + 1) : t.longer + (u - border) / t.each;
 }
 
 // The last b of n with cum[b] <= x (cum[0] <= x < cum[n]).
@@ -108,47 +128,62 @@ constexpr int32_t find(const I* cum, int32_t n, I x) {
 // A run of units of one task.
 struct Segment {
     uint32_t task;               // number among the prefix's, or among the sequences' own tasks
-    uint32_t task_start, units;  // the task's first unit (of all), and its units
+    uint32_t task_start, units;  // where its units begin in the cost of all tasks (behind kTaskUnits); its units
     uint32_t first, end;         // this run, within the task
+    uint32_t offset;             // units of the prefix before the task's chunk
     uint32_t prefix_units;       // units of the prefix that the task begins with
     int32_t kv_head, b, row0;    // b < 0: the prefix, for rows of the whole batch
     int32_t count, length;       // of sequence b
     bool bad;
 };
 
-// The task of unit u.  `find_tile(sequence, at, start)` gives the row tile that
-// holds unit `at` of a sequence and head, and the unit at which it starts.
-template <class FindTile>
-constexpr Segment locate(const Split& a, const Totals& t, const uint32_t* cum_units, uint32_t u, FindTile find_tile) {
+// The task at place u of the cost.  `sequence_of(b)` gives sequence b;
+// `find_tile(sequence, at, start)` the row tile that holds place `at` of a sequence
+// and head, and the place at which that tile's task begins.
+template <class SequenceOf, class FindTile>
+constexpr Segment locate(const Split& a, const Totals& t, const uint32_t* cum_cost, uint32_t u, SequenceOf sequence_of,
+                         FindTile find_tile) {
     Segment g{};
-    if (u < t.prefix_units) {
-        g.task = u / (uint32_t)a.prefix_units;
-        g.task_start = g.task * (uint32_t)a.prefix_units;
-        g.units = g.prefix_units = (uint32_t)a.prefix_units;
-        g.kv_head = (int32_t)(g.task / (uint32_t)t.prefix_tiles);
-        g.row0 = (int32_t)(g.task - (uint32_t)g.kv_head * (uint32_t)t.prefix_tiles) * a.plan.prefix_rows;
+    if (u < t.prefix_cost) {
+        const uint32_t tiles = (uint32_t)t.prefix_tiles, units = (uint32_t)a.prefix_units;
+        const uint32_t head = tiles * (units + t.chunks * kTaskUnits), chunk_cost = (t.chunk + kTaskUnits) * tiles;
+        g.kv_head = (int32_t)(u / head);
+        const uint32_t at = u - (uint32_t)g.kv_head * head, chunk = at / chunk_cost, in_chunk = at - chunk * chunk_cost;
+        g.offset = chunk * t.chunk;
+        g.units = smaller(t.chunk, units - g.offset);
+        const uint32_t tile = in_chunk / (g.units + kTaskUnits);
+        g.task = ((uint32_t)g.kv_head * t.chunks + chunk) * tiles + tile;
+        g.task_start = u - (in_chunk - tile * (g.units + kTaskUnits)) + kTaskUnits;
+        g.prefix_units = units;
+        g.row0 = (int32_t)tile << a.plan.prefix_shift;
         g.b = -1;
         return g;
     }
-    const uint32_t v = u - t.prefix_units;
-    g.b = find(cum_units, a.batch, v);
-    const Sequence s = sequence(a, g.b);
-    const uint32_t base = cum_units[g.b], own = (cum_units[g.b + 1] - base) / (uint32_t)a.kv_heads;
-    g.kv_head = (int32_t)((v - base) / own);
+    const uint32_t v = u - t.prefix_cost;
+    g.b = find(cum_cost, a.batch, v);
+    const Sequence s = sequence_of(g.b);
+    const uint32_t base = cum_cost[g.b], head = (cum_cost[g.b + 1] - base) / (uint32_t)a.kv_heads;
+    g.kv_head = (int32_t)((v - base) / head);
     uint32_t start = 0;
-    const int32_t rt = find_tile(s, v - base - (uint32_t)g.kv_head * own, start);
+    const int32_t rt = find_tile(s, v - base - (uint32_t)g.kv_head * head, start);
     g.task = (uint32_t)(g.b * a.kv_heads + g.kv_head) * (uint32_t)a.plan.own_tiles + (uint32_t)rt;
-    g.task_start = t.prefix_units + base + (uint32_t)g.kv_head * own + start;
+    g.task_start = t.prefix_cost + base + (uint32_t)g.kv_head * head + start + kTaskUnits;
     g.units = tile_units(a, s, rt);
     g.prefix_units = a.plan.joined ? (uint32_t)a.prefix_units : 0u;
-    g.row0 = rt * a.plan.own_rows;
+    g.row0 = rt << a.plan.own_shift;
     g.count = s.count;
     g.length = s.length;
     g.bad = s.bad;
     return g;
 }
+// A workgroup's run of the task that it finds at place u of the cost, its own run
+// ending before place `end`; empty (first == end) if it ends before the task's units.
+constexpr void cut(Segment& g, uint32_t u, uint32_t end) {
+    g.first = u > g.task_start ? u - g.task_start : 0u;
+    g.end = end > g.task_start ? smaller(g.units, end - g.task_start) : 0u;
+}
 
-// The keys of a unit that a wave stages are two runs of 16, each within a page.
+// The keys of a unit that a wave stages are a run of 16, which lies within a page.
 // Run r (0 .. kAttendKeys / 16 - 1) of a unit that begins at key `base`: its
 // first key; behind the last key there is, the run that holds it.
 constexpr int32_t run_start(int32_t base, int32_t r, int32_t last_key) {
@@ -160,9 +195,9 @@ constexpr int32_t own_end(const Split& a, const Segment& g) {
     return g.length + smaller(g.count - 1, (g.row0 + a.plan.own_rows - 1) / a.group) + 1;
 }
 
-// Row place of a segment's part.  With a shared prefix every task's every
-// segment has one: segments in order differ in their task or in their workgroup,
-// and so in the sum of the two.  Else only a cut task's have: a workgroup cuts at
+// Row place of a segment's part.  With a shared prefix every segment of every task
+// has one: segments in order differ in their task or in their workgroup, and so in
+// the sum of the two.  Without one only cut tasks have parts: a workgroup cuts at
 // most the one that it begins in and the one that it ends in.
 constexpr bool whole_task(const Split& a, const Segment& g) {
     return a.plan.joined && g.first == 0 && g.end == g.units;
@@ -173,34 +208,47 @@ constexpr int64_t part_place(const Split& a, const Segment& g, uint32_t w) {
                    : a.plan.own_parts + (int64_t)(g.task + w) * a.plan.own_rows;
 }
 
+// With a shared prefix: part k (0 .. kChunkParts chunks - 1) of row r of a key/value
+// head's prefix rows, or -1 where its task has fewer.  (A chunk has no
+// more units than a workgroup is dealt, so at most one border cuts its tasks.)
+constexpr uint32_t kChunkParts = 2;
+constexpr int64_t prefix_part(const Split& a, const Totals& t, int32_t kv_head, int32_t r, uint32_t k) {
+    const uint32_t tiles = (uint32_t)t.prefix_tiles, tile = (uint32_t)r >> a.plan.prefix_shift;
+    const uint32_t chunk = k / kChunkParts, offset = chunk * t.chunk;
+    const uint32_t units = smaller(t.chunk, (uint32_t)a.prefix_units - offset);
+    const uint32_t start = (uint32_t)kv_head * tiles * ((uint32_t)a.prefix_units + t.chunks * kTaskUnits) +
+                           chunk * (t.chunk + kTaskUnits) * tiles + tile * (units + kTaskUnits) + kTaskUnits;
+    const uint32_t task = ((uint32_t)kv_head * t.chunks + chunk) * tiles + tile;
+    const uint32_t w = group_of(t, start) + (k - chunk * kChunkParts);
+    if (w > group_of(t, start + units - 1)) return -1;
+    return (int64_t)(task + w) * a.plan.prefix_rows + (r & (a.plan.prefix_rows - 1));
+}
+
 // The parts of one row: n of them, from place `first` on in steps.
 struct Parts {
     int64_t first, step;
     int32_t n;
 };
-
-// With a shared prefix: the row's parts of the prefix's task and of its sequence's own.
-constexpr Parts prefix_parts(const Split& a, const Totals& t, int32_t tokens_before, int32_t token, int32_t kv_head,
-                             int32_t g) {
-    const int32_t r = (tokens_before + token) * a.group + g, tile = r / a.plan.prefix_rows;
-    const uint32_t task = (uint32_t)kv_head * (uint32_t)t.prefix_tiles + (uint32_t)tile;
-    const uint32_t start = task * (uint32_t)a.prefix_units;
-    const uint32_t w0 = group_of(t, start), w1 = group_of(t, start + (uint32_t)a.prefix_units - 1);
-    return Parts{(int64_t)(task + w0) * a.plan.prefix_rows + (r - tile * a.plan.prefix_rows), a.plan.prefix_rows,
-                 (int32_t)(w1 - w0) + 1};
-}
-constexpr Parts own_parts(const Split& a, const Totals& t, const Sequence& s, uint32_t units_before, uint32_t units,
+// With a shared prefix: a row's parts of its sequence's own task.
+constexpr Parts own_parts(const Split& a, const Totals& t, const Sequence& s, uint32_t cost_before, uint32_t cost,
                           int32_t b, int32_t token, int32_t kv_head, int32_t g) {
-    const int32_t r = token * a.group + g, tile = r / a.plan.own_rows;
-    uint32_t start = t.prefix_units + units_before + (uint32_t)kv_head * (units / (uint32_t)a.kv_heads);
-    for (int32_t rt = 0; rt < tile; ++rt) start += tile_units(a, s, rt);
+    const int32_t r = token * a.group + g, tile = r >> a.plan.own_shift;
+    uint32_t start = t.prefix_cost + cost_before + (uint32_t)kv_head * (cost / (uint32_t)a.kv_heads) + kTaskUnits;
+    for (int32_t rt = 0; rt < tile; ++rt) start += tile_cost(a, s, rt);
     const uint32_t task = (uint32_t)(b * a.kv_heads + kv_head) * (uint32_t)a.plan.own_tiles + (uint32_t)tile;
     const uint32_t w0 = group_of(t, start), w1 = group_of(t, start + tile_units(a, s, tile) - 1);
-    return Parts{a.plan.own_parts + (int64_t)(task + w0) * a.plan.own_rows + (r - tile * a.plan.own_rows),
+    return Parts{a.plan.own_parts + (int64_t)(task + w0) * a.plan.own_rows + (r - (tile << a.plan.own_shift)),
                  a.plan.own_rows, (int32_t)(w1 - w0) + 1};
 }
 
-// Without one: row r of a task cut by the borders of workgroups w0 .. w1; the
+// Without one: whether the border before workgroup w (w > 0) is the first to cut a
+// task's units, and then the workgroups that have parts of it.
+constexpr bool first_border(const Totals& t, const Segment& g, uint32_t w, uint32_t& w0, uint32_t& w1) {
+    w0 = group_of(t, g.task_start);
+    w1 = group_of(t, g.task_start + g.units - 1);
+    return group_start(t, w) > g.task_start && w == w0 + 1;
+}
+// Row r of a task cut by the borders of workgroups w0 .. w1; the
 // first one's part is its last segment's, the others' are their first ones'.
 constexpr Parts first_cut_part(const Split& a, uint32_t w0, int32_t r) {
     return Parts{(int64_t)(2 * w0 + 1) * a.plan.own_rows + r, 0, 1};

@@ -31,6 +31,7 @@ number of tokens a sequence, as the ragged verification's are.
 from __future__ import annotations
 
 import ctypes
+import struct
 from typing import Optional, Tuple
 
 import torch
@@ -77,6 +78,11 @@ class AttendDesc(ctypes.Structure):
                 ("workspace", _vp), ("workspace_bytes", _sz)]
 
 
+# the same structures, packed in one go: filling a ctypes structure field by
+# field takes as long as the launch itself
+_pack_append = struct.Struct("@QQ6qQQqQ7i4x").pack
+_pack_attend = struct.Struct("@QQ6qQQqQQQQ10ifQN").pack
+
 _lib = None
 
 
@@ -88,8 +94,8 @@ def load_library() -> ctypes.CDLL:
     lib = binding.load_library()
     lib.spec_cache_init.argtypes = [ctypes.POINTER(Tables), _i32, _vp]
     lib.spec_cache_plan.argtypes = [ctypes.POINTER(Tables), _vp, _vp, _vp, _i32, _i32, _vp, _vp, _vp]
-    lib.spec_cache_append.argtypes = [ctypes.POINTER(AppendDesc), _vp]
-    lib.spec_cache_attend.argtypes = [ctypes.POINTER(AttendDesc), _vp]
+    lib.spec_cache_append.argtypes = [_vp, _vp]
+    lib.spec_cache_attend.argtypes = [_vp, _vp]
     for f in (lib.spec_cache_init, lib.spec_cache_plan, lib.spec_cache_append, lib.spec_cache_attend):
         f.restype = ctypes.c_int
     lib.spec_cache_attend_workspace_bytes.argtypes = [_i32] * 5
@@ -98,13 +104,16 @@ def load_library() -> ctypes.CDLL:
     return lib
 
 
-def _call(device_index: int, f, what: str, *args) -> None:
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+def _call(index: int, f, what: str, *args) -> None:
     """f(*args, stream) on the current stream of the tensors' device."""
-    if torch.cuda.current_device() == device_index:
-        st = f(*args, _stream(device_index))
+    if _current_device() == index:
+        st = f(*args, _stream(index))
     else:
-        with torch.cuda.device(device_index):
-            st = f(*args, _stream(device_index))
+        with torch.cuda.device(index):
+            st = f(*args, _stream(index))
     if st != 0:
         _check(st, what)
 
@@ -116,37 +125,36 @@ def _stream(index: int) -> int:
 
 
 def _int32(name: str, t: torch.Tensor, shape, index: int) -> None:
-    if t.dtype != torch.int32 or tuple(t.shape) != shape or not t.is_contiguous() or t.get_device() != index:
+    if t.dtype != torch.int32 or t.shape != shape or not t.is_contiguous() or t.get_device() != index:
         raise SpecVerifyError(f"{name} must be a contiguous int32 {list(shape)} tensor on device {index}")
 
 
-def _rows(name: str, t: torch.Tensor, index: int, dtype) -> None:
-    """A [batch, tokens, heads, head_dim] tensor that the kernels can address."""
-    if t.dim() != 4 or t.get_device() != index or t.dtype != dtype:
-        raise SpecVerifyError(f"{name} must be a {dtype} [batch, tokens, heads, head_dim] tensor on device {index}")
-    if t.stride(3) != 1 or t.stride(0) % 8 or t.stride(1) % 8 or t.stride(2) % 8 or t.data_ptr() % 16:
+def _rows(name: str, t: torch.Tensor, shape, index: int, dtype):
+    """The address and the strides of a [batch, tokens, heads, head_dim] tensor that the kernels can address."""
+    if t.shape != shape or t.get_device() != index or t.dtype != dtype:
+        raise SpecVerifyError(f"{name} must be a {dtype} {list(shape)} tensor on device {index}")
+    at, (sb, st, sh, sd) = t.data_ptr(), t.stride()
+    if sd != 1 or (sb | st | sh) & 7 or at & 15:
         raise SpecVerifyError(f"{name}: head_dim must be dense, the other strides multiples of 8 elements and the data "
                               f"aligned to 16 bytes (strides {t.stride()})")
+    return at, sb, st, sh
 
 
-def _caches(k_cache: torch.Tensor, v_cache: torch.Tensor, kv_heads: Optional[int], head_dim: int) -> int:
-    """Checks a pair of caches; the stride of their pages."""
-    index, dtype = k_cache.get_device(), k_cache.dtype
-    if index < 0 or k_cache.dim() != 4 or dtype not in DTYPE_CODES:
+def _caches(k_cache: torch.Tensor, v_cache: torch.Tensor):
+    """A pair of caches: device, dtype, shape, addresses and the stride of their pages."""
+    index, dtype, shape, strides = k_cache.get_device(), k_cache.dtype, k_cache.shape, k_cache.stride()
+    if index < 0 or len(shape) != 4 or dtype not in DTYPE_CODES:
         raise SpecVerifyError("caches must be float16 or bfloat16 device tensors [num_pages, kv_heads, page_size, "
                               "head_dim]")
-    if v_cache.shape != k_cache.shape or v_cache.dtype != dtype or v_cache.get_device() != index or \
-            v_cache.stride() != k_cache.stride():
+    if v_cache.shape != shape or v_cache.dtype != dtype or v_cache.get_device() != index or v_cache.stride() != strides:
         raise SpecVerifyError("k_cache and v_cache must be alike in shape, strides, dtype and device")
-    n, h, p, d = k_cache.shape
-    if (kv_heads is not None and h != kv_heads) or d != head_dim:
-        raise SpecVerifyError(f"caches of {h} heads of {d} values; expected {kv_heads} of {head_dim}")
-    sn, sh, sp, sd = k_cache.stride()
+    (n, h, p, d), (sn, sh, sp, sd) = shape, strides
     if n == 1:
         sn = max(sn, h * p * d)
-    if (sd, sp) != (1, d) or (h > 1 and sh != p * d) or sn % 8 or k_cache.data_ptr() % 16 or v_cache.data_ptr() % 16:
+    k, v = k_cache.data_ptr(), v_cache.data_ptr()
+    if sd != 1 or sp != d or (h > 1 and sh != p * d) or (sn | k >> 1 | v >> 1) & 7 or (k | v) & 1:
         raise SpecVerifyError("a cache's pages must be dense and aligned to 16 bytes")
-    return sn
+    return index, dtype, shape, k, v, sn
 
 
 def append(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
@@ -154,18 +162,17 @@ def append(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: tor
     """New keys and values ``[B, n, kv_heads, head_dim]`` into the slots that ``slots`` (int32 ``[B, n]``) names;
     tokens with a slot outside the cache (-1) are left out.  Rows may lie apart (views of a fused projection)."""
     lib = _lib if _lib is not None else load_library()
-    if k.dim() != 4 or v.shape != k.shape:
-        raise SpecVerifyError("k and v must be [batch, tokens, kv_heads, head_dim]")
-    B, n, h, d = k.shape
-    page_stride = _caches(k_cache, v_cache, h, d)
-    index = k_cache.get_device()
-    _rows("k", k, index, k_cache.dtype)
-    _rows("v", v, index, k_cache.dtype)
+    index, dtype, (num_pages, h, p, d), k_at, v_at, page_stride = _caches(k_cache, v_cache)
+    shape = k.shape
+    if len(shape) != 4 or shape[2] != h or shape[3] != d:
+        raise SpecVerifyError(f"k and v must be [batch, tokens, {h}, {d}] for these caches; k is {list(shape)}")
+    B, n = shape[0], shape[1]
+    k_from, kb, kt, kh = _rows("k", k, shape, index, dtype)
+    v_from, vb, vt, vh = _rows("v", v, shape, index, dtype)
     _int32("slots", slots, (B, n), index)
-    desc = AppendDesc(k.data_ptr(), v.data_ptr(), _i64x3(*k.stride()[:3]), _i64x3(*v.stride()[:3]),
-                      k_cache.data_ptr(), v_cache.data_ptr(), page_stride, slots.data_ptr(), DTYPE_CODES[k.dtype],
-                      B, n, h, d, k_cache.shape[0], k_cache.shape[2])
-    _call(index, lib.spec_cache_append, "spec_cache_append", ctypes.byref(desc))
+    _call(index, lib.spec_cache_append, "spec_cache_append",
+          _pack_append(k_from, v_from, kb, kt, kh, vb, vt, vh, k_at, v_at, page_stride, slots.data_ptr(),
+                       DTYPE_CODES[dtype], B, n, h, d, num_pages, p))
 
 
 def attend_workspace_bytes(batch: int, max_new: int, q_heads: int, kv_heads: int, head_dim: int) -> int:
@@ -194,13 +201,12 @@ def attend(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, block_
     ``scale`` defaults to ``head_dim ** -0.5``.  ``workspace`` (see new_attend_workspace) avoids an allocation a call.
     """
     lib = _lib if _lib is not None else load_library()
-    if q.dim() != 4:
-        raise SpecVerifyError("q must be [batch, tokens, q_heads, head_dim]")
-    B, n, H, D = q.shape
-    page_stride = _caches(k_cache, v_cache, None, D)
-    index = k_cache.get_device()
-    num_pages, K, P, _ = k_cache.shape
-    _rows("q", q, index, k_cache.dtype)
+    index, dtype, (num_pages, K, P, D), k_at, v_at, page_stride = _caches(k_cache, v_cache)
+    shape = q.shape
+    if len(shape) != 4 or shape[3] != D:
+        raise SpecVerifyError(f"q must be [batch, tokens, q_heads, {D}] for these caches; it is {list(shape)}")
+    B, n, H, _ = shape
+    q_at, qb, qt, qh = _rows("q", q, shape, index, dtype)
     if block_table.dim() != 2:
         raise SpecVerifyError("block_table must be [batch, max_pages]")
     M = block_table.shape[1]
@@ -211,24 +217,21 @@ def attend(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, block_
     if prefix_len:
         if prefix_table is None or prefix_table.dim() != 1 or prefix_table.numel() * P < prefix_len:
             raise SpecVerifyError(f"prefix_table must name the pages of {prefix_len} tokens")
-        _int32("prefix_table", prefix_table, (prefix_table.numel(),), index)
+        _int32("prefix_table", prefix_table, prefix_table.shape, index)
     if out is None:
-        out = torch.zeros(q.shape, dtype=q.dtype, device=q.device) if counts is not None else \
-            torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    else:
-        if out.shape != q.shape:
-            raise SpecVerifyError(f"out must have q's shape {tuple(q.shape)}")
-        _rows("out", out, index, q.dtype)
+        out = torch.empty(shape, dtype=dtype, device=q.device) if counts is None else \
+            torch.zeros(shape, dtype=dtype, device=q.device)
+    out_at, ob, ot, oh = _rows("out", out, shape, index, dtype)
     if workspace is None:
         workspace = new_attend_workspace(B, n, H, K, D, q.device)
     elif not workspace.is_contiguous() or workspace.get_device() != index:
         raise SpecVerifyError(f"workspace must be a contiguous tensor on device {index}")
-    desc = AttendDesc(q.data_ptr(), out.data_ptr(), _i64x3(*q.stride()[:3]), _i64x3(*out.stride()[:3]),
-                      k_cache.data_ptr(), v_cache.data_ptr(), page_stride, block_table.data_ptr(),
-                      lengths.data_ptr(), _ptr(counts), _ptr(prefix_table), prefix_len, DTYPE_CODES[q.dtype], B, n, H,
-                      K, D, M, num_pages, P, D ** -0.5 if scale is None else scale, workspace.data_ptr(),
-                      workspace.numel() * workspace.element_size())
-    _call(index, lib.spec_cache_attend, "spec_cache_attend", ctypes.byref(desc))
+    _call(index, lib.spec_cache_attend, "spec_cache_attend",
+          _pack_attend(q_at, out_at, qb, qt, qh, ob, ot, oh, k_at, v_at, page_stride, block_table.data_ptr(),
+                       lengths.data_ptr(), 0 if counts is None else counts.data_ptr(),
+                       prefix_table.data_ptr() if prefix_len else 0, prefix_len, DTYPE_CODES[dtype], B, n, H, K, D, M,
+                       num_pages, P, D ** -0.5 if scale is None else scale, workspace.data_ptr(),
+                       workspace.numel() * workspace.element_size()))
     return out
 
 

@@ -43,7 +43,7 @@ struct Case {
 static int32_t find_tile_host(const Split& a, const Sequence& s, uint32_t at, uint32_t& start) {
     start = 0;
     for (int32_t rt = 0; rt < a.plan.own_tiles; ++rt) {
-        const uint32_t n = tile_units(a, s, rt);
+        const uint32_t n = tile_cost(a, s, rt);
         if (at < start + n) return rt;
         start += n;
     }
@@ -75,30 +75,36 @@ static void simulate(const Case& c, int id) {
     CHECK(plan.cum_bytes % 16 == 0 && plan.rows % 4 == 0, "case %d", id);  // the parts lie on 16 bytes
     const Split a = make_split(d, plan);
     std::vector<int32_t> cum_tokens(c.batch + 1, 0);
-    std::vector<uint32_t> cum_units(c.batch + 1, 0);
+    std::vector<uint32_t> cum_cost(c.batch + 1, 0);
     for (int32_t b = 0; b < c.batch; ++b) {
         const Sequence s = sequence(a, b);
         cum_tokens[b + 1] = cum_tokens[b] + s.count;
-        cum_units[b + 1] = cum_units[b] + sequence_units(a, s) * (uint32_t)c.kv_heads;
+        uint32_t cost = 0;
+        for (int32_t rt = 0; rt < plan.own_tiles; ++rt) cost += tile_cost(a, s, rt);
+        cum_cost[b + 1] = cum_cost[b] + cost * (uint32_t)c.kv_heads;
     }
-    const Totals t = totals(a, cum_tokens[c.batch], cum_units[c.batch]);
+    const Totals t = totals(a, cum_tokens[c.batch], cum_cost[c.batch]);
     // the segments of each task, in order: by (prefix's?, task)
     std::map<std::pair<bool, uint32_t>, std::vector<Got>> got;
     std::map<std::pair<bool, uint32_t>, Segment> tasks;
     std::vector<std::pair<int64_t, int64_t>> places;
     uint32_t covered = 0;
+    std::map<std::pair<bool, uint32_t>, uint32_t> done;  // units of each task
     for (uint32_t w = 0; w < t.groups; ++w) {
         const uint32_t end = group_start(t, w + 1);
         uint32_t u = group_start(t, w);
         CHECK(u == covered && u < end, "case %d: group %u", id, w);
-        int segments = 0;
+        covered = end;
         while (u < end) {
             CHECK(group_of(t, u) == w, "case %d: unit %u", id, u);
-            Segment g = locate(a, t, cum_units.data(), u,
-                               [&](const Sequence& s, uint32_t at, uint32_t& start) { return find_tile_host(a, s, at, start); });
-            CHECK(u >= g.task_start && u < g.task_start + g.units, "case %d: unit %u", id, u);
-            g.first = u - g.task_start;
-            g.end = smaller(g.units, end - g.task_start);
+            Segment g = locate(
+                a, t, cum_cost.data(), u, [&](int32_t b) { return sequence(a, b); },
+                [&](const Sequence& s, uint32_t at, uint32_t& start) { return find_tile_host(a, s, at, start); });
+            CHECK(u + kTaskUnits >= g.task_start && u < g.task_start + g.units && g.units > 0, "case %d: unit %u", id, u);
+            cut(g, u, end);
+            if (g.first == g.end) break;
+            CHECK(g.first < g.end && g.end <= g.units && g.first == done[std::make_pair(g.b < 0, g.task)], "case %d", id);
+            done[std::make_pair(g.b < 0, g.task)] = g.end;
             const int32_t rows = g.b < 0 ? plan.prefix_rows : plan.own_rows;
             if (!whole_task(a, g)) {
                 const int64_t place = part_place(a, g, w);
@@ -107,7 +113,7 @@ static void simulate(const Case& c, int id) {
                 got[{g.b < 0, g.task}].push_back({g.first, g.end, place});
             }
             tasks[{g.b < 0, g.task}] = g;
-            for (uint32_t k = g.first; k < g.end; ++k) {
+            for (uint32_t k = g.offset + g.first; k < g.offset + g.end; ++k) {
                 const bool pre = k < g.prefix_units;
                 const int32_t base = (int32_t)(pre ? k : k - g.prefix_units) * kAttendKeys;
                 const int32_t last = pre ? c.prefix_len - 1 : own_end(a, g) - 1;
@@ -123,11 +129,10 @@ static void simulate(const Case& c, int id) {
                 }
             }
             u = g.task_start + g.end;
-            ++segments;
         }
-        covered = end;
     }
-    CHECK(covered == t.units, "case %d", id);
+    CHECK(covered == t.cost, "case %d", id);
+    for (const auto& x : tasks) CHECK(done[x.first] == x.second.units, "case %d: a task not done", id);
     std::sort(places.begin(), places.end());
     for (size_t i = 1; i < places.size(); ++i) CHECK(places[i - 1].second <= places[i].first, "case %d", id);
 
@@ -154,24 +159,41 @@ static void simulate(const Case& c, int id) {
                     CHECK(g.units - g.prefix_units >= need, "case %d", id);
                     CHECK(own_common(a, g) <= s.length + token + 1 && s.length + token < own_end(a, g), "case %d", id);
                     if (!plan.joined) {
-                        const Parts pp = prefix_parts(a, t, cum_tokens[b], token, kv, h);
                         const int32_t flat = (cum_tokens[b] + token) * a.group + h;
-                        const uint32_t ptask = (uint32_t)(kv * t.prefix_tiles + flat / plan.prefix_rows);
-                        CHECK((size_t)pp.n == got[std::make_pair(true, ptask)].size(), "case %d", id);
-                        same(pp, got[std::make_pair(true, ptask)], 0, flat % plan.prefix_rows);
+                        uint32_t keys = 0;  // units of the prefix that its parts hold
+                        for (uint32_t chunk = 0; chunk < t.chunks; ++chunk) {
+                            const uint32_t ptask =
+                                ((uint32_t)kv * t.chunks + chunk) * t.prefix_tiles + flat / plan.prefix_rows;
+                            const auto& have = got[std::make_pair(true, ptask)];
+                            CHECK(have.size() == 1 || have.size() == 2, "case %d", id);
+                            CHECK(tasks.at({true, ptask}).offset == keys, "case %d", id);
+                            for (uint32_t k = 0; k < 2; ++k) {
+                                const int64_t place = prefix_part(a, t, kv, flat, 2 * chunk + k);
+                                CHECK((place >= 0) == (k < have.size()), "case %d", id);
+                                if (place < 0) continue;
+                                CHECK(place == have[k].place + flat % plan.prefix_rows, "case %d", id);
+                                keys += have[k].end - have[k].first;
+                            }
+                        }
+                        CHECK(keys == (uint32_t)a.prefix_units, "case %d", id);
                         const Parts op =
-                            own_parts(a, t, s, cum_units[b], cum_units[b + 1] - cum_units[b], b, token, kv, h);
+                            own_parts(a, t, s, cum_cost[b], cum_cost[b + 1] - cum_cost[b], b, token, kv, h);
                         CHECK((size_t)op.n == got[std::make_pair(false, task)].size(), "case %d", id);
                         same(op, got[std::make_pair(false, task)], 0, r % plan.own_rows);
                     } else if (got.count({false, task})) {
-                        const uint32_t w0 = group_of(t, g.task_start), w1 = group_of(t, g.task_start + g.units - 1);
                         const auto& have = got[std::make_pair(false, task)];
+                        uint32_t w0 = 0, w1 = 0;
+                        CHECK(first_border(t, g, group_of(t, g.task_start) + 1, w0, w1), "case %d", id);
                         CHECK(w1 > w0 && have.size() == w1 - w0 + 1, "case %d", id);
                         same(first_cut_part(a, w0, r % plan.own_rows), have, 0, r % plan.own_rows);
                         same(later_cut_parts(a, w0, w1, r % plan.own_rows), have, 1, r % plan.own_rows);
-                        // one workgroup of the joining kernel takes it: the border before w0 + 1
-                        CHECK(group_start(t, w0 + 1) > g.task_start && group_start(t, w0 + 1) < g.task_start + g.units,
-                              "case %d", id);
+                        // one workgroup of the joining kernel takes it
+                        for (uint32_t w = 1; w < t.groups && r % plan.own_rows == 0; ++w) {
+                            const uint32_t u = group_start(t, w);
+                            if (u + kTaskUnits < g.task_start || u >= g.task_start + g.units) continue;
+                            uint32_t x0, x1;
+                            CHECK(first_border(t, g, w, x0, x1) == (w == w0 + 1), "case %d", id);
+                        }
                     } else {
                         CHECK(group_of(t, g.task_start) == group_of(t, g.task_start + g.units - 1), "case %d", id);
                     }

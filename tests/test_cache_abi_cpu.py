@@ -59,6 +59,15 @@ def test_structures_are_the_headers(tmp_path):
     for cls, _ in pairs:
         want += [ctypes.sizeof(cls)] + [getattr(cls, f[0]).offset for f in cls._fields_]
     assert got == want
+    # and what the binding packs in one go
+    i3 = ctypes.c_int64 * 3
+    a = list(range(1, 20))
+    d = AppendDesc(1, 2, i3(3, 4, 5), i3(6, 7, 8), *a[8:])
+    assert bytes(d) == paged_cache._pack_append(*a)
+    a = list(range(1, 29))
+    a[25] = 0.75                                             # scale
+    d = AttendDesc(1, 2, i3(3, 4, 5), i3(6, 7, 8), *a[8:])
+    assert bytes(d) == paged_cache._pack_attend(*a)
 
 
 def _tables(**kw):
