@@ -80,6 +80,14 @@ struct AttendArgs {
 __device__ __forceinline__ int32_t uniform(int32_t x) { return __builtin_amdgcn_readfirstlane(x); }
 __device__ __forceinline__ uint32_t uniform(uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); }
 
+// The same value, of which the compiler knows nothing: what is computed from it is
+// computed there, not kept in registers from before.
+template <class X>
+__device__ __forceinline__ X forget(X x) {
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // max or sum over the two halves of the wave, in every lane
@@ -168,14 +176,14 @@ __device__ __forceinline__ Totals sum_batch(const Split& a, const Batch& batch, 
 __device__ __forceinline__ int32_t find_tile(const Split& a, const Sequence& s, uint32_t at, uint32_t& start) {
     start = 0;
     if (a.plan.own_tiles == 1) return 0;
-    const int lane = threadIdx.x & 63;
+    const int lane = forget((int)threadIdx.x) & 63;
     uint32_t before = 0;
     for (int32_t base = 0; base < a.plan.own_tiles; base += 64) {
         const uint32_t own = (base + lane < a.plan.own_tiles) ? tile_cost(a, s, base + lane) : 0u;
         uint32_t end = own;
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
-            const uint32_t o = __shfl_up(end, d);
+            const uint32_t o = (uint32_t)__builtin_amdgcn_ds_bpermute((lane - d) * 4, (int)end);
             if (lane >= d) end += o;
         }
         const uint64_t over = __ballot(before + end > at);
@@ -189,13 +197,8 @@ __device__ __forceinline__ int32_t find_tile(const Split& a, const Sequence& s, 
     return 0;  // (not reached: `at` is below the sum of all tiles)
 }
 
-// The task at place u of the cost, in scalar registers.
-template <class SequenceOf>
-__device__ __forceinline__ Segment task_at(const Split& a, const Totals& t, const uint32_t* cum_cost, uint32_t u,
-                                           SequenceOf sequence_of) {
-    Segment g = locate(a, t, cum_cost, u, sequence_of, [&](const Sequence& s, uint32_t at, uint32_t& start) {
-        return find_tile(a, s, at, start);
-    });
+// A task, in scalar registers.
+__device__ __forceinline__ Segment uniform(Segment g) {
     g.task = uniform(g.task);
     g.task_start = uniform(g.task_start);
     g.units = uniform(g.units);
@@ -209,6 +212,19 @@ __device__ __forceinline__ Segment task_at(const Split& a, const Totals& t, cons
     g.bad = uniform((int32_t)g.bad) != 0;
     return g;
 }
+template <class SequenceOf>
+__device__ __forceinline__ Segment own_task_at(const Split& a, const uint32_t* cum_cost, uint32_t u, SequenceOf sequence_of) {
+    return uniform(own_task(a, cum_cost, u, sequence_of, [&](const Sequence& s, uint32_t at, uint32_t& start) {
+        return find_tile(a, s, at, start);
+    }));
+}
+
+// What a workgroup's tasks are.
+enum Kind : int {
+    kShared,  // the prefix's, for rows of the whole batch
+    kOwn,     // the sequences' own keys
+    kJoined   // both in one task, first the prefix
+};
 
 // ---------------------------------------------------------------------------
 // one segment
@@ -257,13 +273,6 @@ __device__ __forceinline__ void stage_barrier() {
     asm volatile("" : : : "memory");
 }
 
-// The same value, of which the compiler knows nothing: what is computed from it is
-// computed there, not kept in registers from before.
-__device__ __forceinline__ int forget(int x) {
-    asm volatile("" : "+v"(x));
-    return x;
-}
-
 // Nothing is moved across: the reads written before a block of matrix products are
 // issued before it, so that their latency passes behind it.
 __device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }
@@ -279,11 +288,12 @@ __device__ __forceinline__ void lds_barrier() {
 
 // Whether this thread's share of a tile holds infinities or NaN; `clear` makes them zeros.
 template <class T, int D>
-__device__ __forceinline__ int special_chunks(char* tile, bool clear) {
+__device__ __forceinline__ bool special_chunks(char* tile, bool clear) {
     using S = Shape<D>;
     uint32_t found = 0;
+    const uint32_t ones = forget(~0u);
 #pragma unroll 1
-    for (int at = forget(threadIdx.x) * 16; at < S::kTile; at += kThreads * 16) {
+    for (int at = forget((int)threadIdx.x) * 16; at < S::kTile; at += kThreads * 16) {
         // (a chunk behind head_dim holds what was there before: nothing reads it)
         if (D != S::kPitch && (((at / 16) % S::kChunks) ^ swizzle<D>(at / (S::kPitch * 2))) * 8 >= D) continue;
         u32x4 x = *(u32x4*)(tile + at);
@@ -291,14 +301,116 @@ __device__ __forceinline__ int special_chunks(char* tile, bool clear) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const bool low = T::special(x[i] & 0xffffu), high = T::special(x[i] >> 16);
-            x[i] &= (low ? 0u : 0xffffu) | (high ? 0u : 0xffff0000u);
+            x[i] &= (low ? 0u : ones >> 16) | (high ? 0u : ones << 16);
             here |= (uint32_t)low | (uint32_t)high;
         }
         if (clear && here) *(u32x4*)(tile + at) = x;
         found |= here;
     }
-    return (int)found;
+    return found != 0;
 }
+
+// A workgroup's way through its run of the work: the segment at hand, and the
+// pages that this wave stages of it, a run of 16 rows of each unit.
+template <int D, Kind kKind>
+struct Work {
+    using S = Shape<D>;
+    const AttendArgs& a;
+    const Totals& t;
+    const Batch& batch;
+    const uint32_t lds;         // LDS address of the tiles
+    const uint32_t group, end;  // this workgroup, and where its run of the cost ends
+    Segment g;                  // first .. end: units of the task's keys
+    int64_t place;              // of its part
+    bool whole;                 // it is the whole task, and has no part
+    uint32_t at;                // place in the cost behind it
+    uint32_t paged;             // lane l has the place in the caches of this wave's rows of unit `paged` + l
+    uint32_t row_low, row_high;
+    bool poison;                // (one of them would have been on a page that there is not)
+
+    // To the next segment; false if there is none.
+    __device__ __forceinline__ bool advance() {
+        if (at >= end) return false;
+        if constexpr (kKind == kShared)
+            g = uniform(prefix_task(a.split, t, at));
+        else
+            g = own_task_at(a.split, batch.cum_cost, at, [&](int32_t b) { return sequence(batch, b); });
+        cut(g, at, end);
+        if (g.first == g.end) return false;  // (the run ends within the task's cost of starting)
+        whole = kKind == kJoined && whole_task(a.split, g);
+        place = part_place(a.split, g, group);
+        at = g.task_start + g.end;
+        g.first += g.offset;
+        g.end += g.offset;
+        poison = g.bad;
+        paged = g.first;
+        look_up();
+        return true;
+    }
+    // Whether unit u is of the prefix, its first key there or in the sequence, and the last key that there is.
+    __device__ __forceinline__ bool in_prefix(uint32_t u) const {
+        return kKind == kShared || (kKind == kJoined && u < g.prefix_units);
+    }
+    __device__ __forceinline__ int first_key(uint32_t u) const {
+        return (int)(kKind != kJoined || u < g.prefix_units ? u : u - g.prefix_units) * kKeys;
+    }
+    __device__ __forceinline__ int last_key(bool prefix) const {
+        return prefix ? a.prefix_len - 1 : own_end(a.split, g) - 1;
+    }
+    __device__ __forceinline__ void look_up() {
+        const int lane = forget((int)threadIdx.x) & 63, wave = uniform((int32_t)(threadIdx.x >> 6));
+        const uint32_t u = smaller(paged + lane, g.end - 1);
+        const bool prefix = in_prefix(u);
+        const int32_t* const table = prefix ? a.prefix_table : a.block_table + (int64_t)max(g.b, 0) * a.split.max_pages;
+        const int first = run_start(first_key(u), wave, last_key(prefix));
+        int page = (prefix || !g.bad) ? table[first >> a.split.page_shift] : 0;
+        if ((uint32_t)page >= (uint32_t)a.num_pages) {
+            page = 0;
+            poison = true;
+        }
+        const int64_t row = (int64_t)page * a.page_stride + (int64_t)(g.kv_head << a.split.page_shift) * D +
+                            (first & ((1 << a.split.page_shift) - 1)) * D;
+        row_low = (uint32_t)row;
+        row_high = (uint32_t)(row >> 32);
+    }
+    // This wave's first row of unit u, in the caches.
+    __device__ __forceinline__ int64_t row_of(uint32_t u) {
+        if (u - paged == 64) {
+            paged = u;
+            look_up();
+        }
+        const uint32_t low = (uint32_t)__builtin_amdgcn_readlane((int)row_low, (int)(u - paged));
+        const uint32_t high = (uint32_t)__builtin_amdgcn_readlane((int)row_high, (int)(u - paged));
+        return (int64_t)((uint64_t)high << 32 | low);
+    }
+    // And the last of its 16 rows that there is: those behind repeat it.
+    __device__ __forceinline__ int last_row(uint32_t u) const {
+        const int last = last_key(in_prefix(u));
+        return last - run_start(first_key(u), uniform((int32_t)(threadIdx.x >> 6)), last);
+    }
+    // This wave's 16 rows of a unit of K (V), to its place in LDS.
+    template <bool kFull>
+    __device__ __forceinline__ void stage(const uint16_t* cache, int64_t row, int last, uint32_t to) const {
+        const uint32_t lane = (uint32_t)forget((int)threadIdx.x) & 63;
+        const int load_row = (int)(lane / S::kChunks), load_chunk = (int)(lane % S::kChunks);
+        const int wave = uniform((int32_t)(threadIdx.x >> 6));
+#pragma unroll
+        for (int j = 0; j < S::kLoads; ++j) {
+            const int in_run = j * S::kRowsLoad + load_row;
+            const int chunk = load_chunk ^ swizzle<D>(load_row) ^ swizzle<D>(j * S::kRowsLoad);
+            const uint32_t offset = (uint32_t)((kFull ? load_row : min(in_run, last)) * D + chunk * 8) * 2;
+            if (D == S::kPitch || chunk * 8 < D)
+                load_to_lds(lds + to + wave * (16 * S::kPitch * 2) + j * 1024,
+                            cache + row + (kFull ? j * S::kRowsLoad * D : 0), offset);
+        }
+    }
+    __device__ __forceinline__ void stage_first() {
+        const int64_t row = row_of(g.first);
+        const int last = last_row(g.first);
+        stage<false>(a.k_cache, row, last, 0);
+        stage<false>(a.v_cache, row, last, S::kTile);
+    }
+};
 
 // The part of a task's rows over a run of its units.  The four waves are WR x WK x
 // WD: WR split the rows (32 each), WK a unit's blocks of 32 keys, and WD the
@@ -316,9 +428,9 @@ __device__ __forceinline__ int special_chunks(char* tile, bool clear) {
 // vector units, the matrix units make the next one's scores, product by product in
 // between (the two overlap in one wave only if its instructions alternate).  Both
 // are staged two deep in LDS, with one barrier between units.
-template <class T, int D, int WR>
-__device__ void segment(const AttendArgs& a, const Segment& g, const int32_t* cum_tokens, char* smem,
-                        float (*wave_stats)[2][32], int* poison_flag, bool whole, int64_t place) {
+template <class T, int D, int WR, Kind kKind>
+__device__ __forceinline__ bool segment(Work<D, kKind>& work, char* smem, float (*wave_stats)[2][32], int* poison_flag,
+                                        int* special_flag) {
     using S = Shape<D>;
     using V8 = typename T::V8;
     constexpr int WK = WR == 4 ? 1 : 2, WD = 4 / (WR * WK);
@@ -332,7 +444,9 @@ __device__ void segment(const AttendArgs& a, const Segment& g, const int32_t* cu
     const int tid = threadIdx.x, lane = forget(tid & 63), half = lane >> 5;
     const int wave = uniform(tid >> 6);
     const int wr = wave % WR, wk = wave / WR % WK, wd = wave / (WR * WK);
-    const uint32_t lds = (uint32_t)(uintptr_t)(SV_LDS char*)smem;
+    const AttendArgs& a = work.a;
+    const Segment g = work.g;
+    const int32_t* const cum_tokens = work.batch.cum_tokens;
 
     // the row of this lane
     struct Row {
@@ -343,7 +457,7 @@ __device__ void segment(const AttendArgs& a, const Segment& g, const int32_t* cu
         const int row = g.row0 + wr * 32 + (lane & 31);
         const int flat = (int)((uint32_t)row / (uint32_t)a.split.group);
         Row r{g.b, flat, g.kv_head * a.split.group + (row - flat * a.split.group), flat < g.count};
-        if (g.b < 0) {
+        if (kKind == kShared) {
             r.live = flat < cum_tokens[a.split.batch];
             r.b = r.live ? find(cum_tokens, a.split.batch, flat) : 0;
             r.token = r.live ? flat - cum_tokens[r.b] : 0;
@@ -352,55 +466,9 @@ __device__ void segment(const AttendArgs& a, const Segment& g, const int32_t* cu
     };
     const Row mine = row_of(lane);
     const int own_limit = g.length + mine.token + 1;  // keys of its own that this row sees
-    const int own_first = own_common(a.split, g), own_last = own_end(a.split, g) - 1;
-
-    // Pages, 64 units ahead: lane l has the page of this wave's run of unit `paged` + l.
-    bool poison = g.bad;
-    uint32_t paged = g.first;
-    int pages;
-    auto look_up = [&]() {
-        const uint32_t u = smaller(paged + lane, g.end - 1);
-        const bool pre = u < g.prefix_units;
-        const int32_t* const table = pre ? a.prefix_table : a.block_table + (int64_t)max(g.b, 0) * a.split.max_pages;
-        const int first = run_start((int)(pre ? u : u - g.prefix_units) * kKeys, wave, pre ? a.prefix_len - 1 : own_last);
-        pages = (pre || !g.bad) ? table[first >> a.split.page_shift] : 0;
-        if ((uint32_t)pages >= (uint32_t)a.num_pages) {
-            pages = 0;
-            poison = true;
-        }
-    };
-    look_up();
-    const int64_t head_at = (int64_t)(g.kv_head << a.split.page_shift) * D;
-    struct Run {
-        int64_t at;  // of its first row, in the caches
-        int last;    // its last row; those behind repeat it
-    };
-    auto run_of = [&](uint32_t u) {
-        if (u - paged == 64) {
-            paged = u;
-            look_up();
-        }
-        const bool pre = u < g.prefix_units;
-        const int last = pre ? a.prefix_len - 1 : own_last;
-        const int first = run_start((int)(pre ? u : u - g.prefix_units) * kKeys, wave, last);
-        const int page = __builtin_amdgcn_readlane(pages, (int)(u - paged));
-        return Run{(int64_t)page * a.page_stride + head_at + (first & ((1 << a.split.page_shift) - 1)) * D, last - first};
-    };
-    // This wave's 16 rows of a unit of K (V), to its place in LDS.
-    auto stage = [&](const uint16_t* cache, const Run& run, uint32_t to) {
-        const int load_row = forget(lane) / S::kChunks, load_chunk = forget(lane) % S::kChunks;
-#pragma unroll
-        for (int j = 0; j < S::kLoads; ++j) {
-            const int in_run = j * S::kRowsLoad + load_row;
-            const int chunk = load_chunk ^ swizzle<D>(in_run);
-            const uint32_t offset = (uint32_t)(min(in_run, run.last) * D + chunk * 8) * 2;
-            if (D == S::kPitch || chunk * 8 < D)
-                load_to_lds(to + wave * (16 * S::kPitch * 2) + j * 1024, cache + run.at, offset);
-        }
-    };
-    Run run = run_of(g.first);
-    stage(a.k_cache, run, lds);
-    stage(a.v_cache, run, lds + S::kTile);
+    const int own_first = kKind == kShared ? 0 : own_common(a.split, g);
+    // (of the segment at hand, not of the one that `work` has turned to)
+    auto in_prefix = [&](uint32_t u) { return kKind == kShared || (kKind == kJoined && u < g.prefix_units); };
 
     V8 q[S::kSteps];
     {
@@ -414,9 +482,7 @@ __device__ void segment(const AttendArgs& a, const Segment& g, const int32_t* cu
         }
     }
     f32x16 o[kPieces];
-#pragma unroll
-    for (int i = 0; i < kPieces; ++i) o[i] = f32x16(0.0f);
-    float top = -INFINITY, sum = 0.0f;  // top: scores as they come from the product
+    float top, sum = 0.0f;  // top: scores as they come from the product
 
     // Places of this lane's reads.  The swizzle flips bits of the chunk's number
     // only, so a read's constant part comes by an exclusive or (chunk) or as an
@@ -433,28 +499,31 @@ __device__ void segment(const AttendArgs& a, const Segment& g, const int32_t* cu
     }
 
     // Key 0 of unit u, the keys that this row sees of its sequence or prefix, and whether a row sees less than all.
-    auto base_of = [&](uint32_t u) { return (int)(u < g.prefix_units ? u : u - g.prefix_units) * kKeys; };
-    auto limit_of = [&](uint32_t u) { return u < g.prefix_units ? a.prefix_len : own_limit; };
+    auto base_of = [&](uint32_t u) { return (int)(kKind != kJoined || in_prefix(u) ? u : u - g.prefix_units) * kKeys; };
+    auto limit_of = [&](uint32_t u) { return in_prefix(u) ? a.prefix_len : own_limit; };
     auto partial_of = [&](uint32_t u) {
-        return base_of(u) + kKeys > (u < g.prefix_units ? a.prefix_len : own_first);
+        return base_of(u) + kKeys > (in_prefix(u) ? a.prefix_len : own_first);
     };
     auto k_read = [&](const char* tile, int m) {  // K's rows and columns of product m
         return *(const V8*)(tile + (k_at ^ (m / NS * 32)) + m % NS * (32 * S::kPitch * 2));
     };
-    // Masks unit u's scores, finds their maximum and moves the reference of the weights to it: they stay relative to
-    // a maximum of earlier units as long as the new one is within 2^8 of it, so nothing is rescaled for small rises.
-    auto refer = [&](uint32_t u, f32x16(&p)[NS], float most) {
-        if (partial_of(u)) {
-            const int key = base_of(u) + wk * NS * 32 + 4 * half, limit = limit_of(u);
-            most = -INFINITY;
+    // Unit u's scores of keys that a row does not see, and then their maximum.
+    auto mask = [&](uint32_t u, f32x16(&p)[NS]) {
+        const int key = base_of(u) + wk * NS * 32 + 4 * half, limit = limit_of(u);
+        float most = -INFINITY;
 #pragma unroll
-            for (int s = 0; s < NS; ++s)
+        for (int s = 0; s < NS; ++s)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {  // key of register i: 8 (i / 4) + 4 half + i % 4
-                    p[s][i] = key + s * 32 + 8 * (i / 4) + i % 4 < limit ? p[s][i] : -INFINITY;
-                    most = fmaxf(most, p[s][i]);
-                }
-        }
+            for (int i = 0; i < 16; ++i) {  // key of register i: 8 (i / 4) + 4 half + i % 4
+                p[s][i] = key + s * 32 + 8 * (i / 4) + i % 4 < limit ? p[s][i] : -INFINITY;
+                most = fmaxf(most, p[s][i]);
+            }
+        return most;
+    };
+    // Moves the reference of the weights to unit u's maximum: they stay relative to a maximum of earlier units as
+    // long as the new one is within 2^8 of it, so nothing is rescaled for small rises.
+    auto refer = [&](auto full, uint32_t u, f32x16(&p)[NS], float most) {
+        if (!decltype(full)::value && partial_of(u)) most = mask(u, p);
         most = halves_max(most);
         if (__any(most > top + a.lazy)) {
             const float now = fmaxf(top, most);
@@ -466,12 +535,15 @@ __device__ void segment(const AttendArgs& a, const Segment& g, const int32_t* cu
         }
     };
     // One unit: p's scores are masked and referred to; `next` gets the scores of the unit after it.  The segment's
-    // even units lie in the first two tiles of LDS (K, V), its odd ones in the others.
-    auto step = [&](uint32_t u, auto odd, f32x16(&p)[NS], f32x16(&next)[NS]) {
+    // even units lie in the first two tiles of LDS (K, V), its odd ones in the others.  `full`: it and the two units
+    // behind it are of the same segment, of one table, and every row sees all their keys.
+    int64_t row = 0;  // this wave's first row of the unit whose K was staged last
+    auto step = [&](auto full, uint32_t u, auto odd, f32x16(&p)[NS], f32x16(&next)[NS]) {
+        constexpr bool kFull = decltype(full)::value;
         constexpr int kHere = decltype(odd)::value * S::kStage, kThere = S::kStage - kHere;
-        const bool more = u + 1 < g.end;
+        const bool more = kFull || u + 1 < g.end;
         char* const v_tile = smem + kHere + S::kTile;
-        const float shift = (top == -INFINITY) ? 0.0f : -top * a.scale_log2;
+        float shift = (top == -INFINITY) ? 0.0f : -top * a.scale_log2;
         float add = 0.0f;
         auto weigh = [&](int from, int to) {
 #pragma unroll
@@ -483,10 +555,11 @@ __device__ void segment(const AttendArgs& a, const Segment& g, const int32_t* cu
 
         stage_barrier();  // K of the next unit and V of this one are there, and every wave has done with those before
         if (more) {
-            stage(a.v_cache, run, lds + kThere + S::kTile);
-            if (u + 2 < g.end) {
-                run = run_of(u + 2);
-                stage(a.k_cache, run, lds + kHere);
+            shift = forget(shift);  // (else the weights' arguments are made before this branch, for both)
+            work.template stage<kFull>(a.v_cache, row, kFull ? 0 : work.last_row(u + 1), kThere + S::kTile);
+            if (kFull || u + 2 < g.end) {
+                row = work.row_of(u + 2);
+                work.template stage<kFull>(a.k_cache, row, kFull ? 0 : work.last_row(u + 2), kHere);
             }
             const char* const tile = smem + kThere;
             V8 k[kAhead + 1];
@@ -507,7 +580,13 @@ __device__ void segment(const AttendArgs& a, const Segment& g, const int32_t* cu
         }
         sum += add;
 
-        if (partial_of(u) && __syncthreads_or(special_chunks<T, D>(v_tile, false))) {
+        bool special = false;
+        if (!kFull && partial_of(u)) {
+            if (__any(special_chunks<T, D>(v_tile, false))) *special_flag = 1;
+            lds_barrier();
+            special = uniform(*special_flag) != 0;
+        }
+        if (special) {
             // A masked key's weight is 0, but 0 times an infinity or NaN is not.
             // Rows take such values from the keys that they see, here; then they
             // are zeros for the product.
@@ -528,9 +607,10 @@ __device__ void segment(const AttendArgs& a, const Segment& g, const int32_t* cu
                         }
                     }
             }
-            __syncthreads();
+            lds_barrier();
             special_chunks<T, D>(v_tile, true);
-            __syncthreads();
+            if (tid == 0) *special_flag = 0;
+            lds_barrier();
         }
         // product m: 16 keys (m / kPieces) for one piece of the output
         auto v_read = [&](int m) {
@@ -561,34 +641,57 @@ __device__ void segment(const AttendArgs& a, const Segment& g, const int32_t* cu
             for (int i = m * NS * 16 / kMmasV; i < (m + 1) * NS * 16 / kMmasV; ++i) most = fmaxf(most, next[i / 16][i % 16]);
         }
         in_order();
-        if (more) refer(u + 1, next, most);
+        if (more) refer(full, u + 1, next, most);
     };
 
     f32x16 scores[2][NS];
     {
-        stage_barrier();  // the first unit's K
+        stage_barrier();  // the first unit
         if (g.first + 1 < g.end) {
-            run = run_of(g.first + 1);
-            stage(a.k_cache, run, lds + S::kStage);
+            row = work.row_of(g.first + 1);
+            work.template stage<false>(a.k_cache, row, work.last_row(g.first + 1), S::kStage);
         }
         float most = -INFINITY;
 #pragma unroll
-        for (int s = 0; s < NS; ++s) scores[0][s] = scores[1][s] = f32x16(0.0f);
+        for (int s = 0; s < NS; ++s) scores[0][s] = f32x16(0.0f);
+        V8 k[kAhead + 1];
 #pragma unroll
-        for (int m = 0; m < kMmas; ++m) scores[0][m % NS] = T::mma(k_read(smem, m), q[m / NS], scores[0][m % NS]);
+        for (int m = 0; m < kAhead; ++m) k[m] = k_read(smem, m);
+#pragma unroll
+        for (int m = 0; m < kMmas; ++m) {
+            in_order();
+            if (m + kAhead < kMmas) k[(m + kAhead) % (kAhead + 1)] = k_read(smem, m + kAhead);
+            scores[0][m % NS] = T::mma(k[m % (kAhead + 1)], q[m / NS], scores[0][m % NS]);
+        }
+        in_order();
 #pragma unroll
         for (int s = 0; s < NS; ++s)
 #pragma unroll
             for (int i = 0; i < 16; ++i) most = fmaxf(most, scores[0][s][i]);
-        refer(g.first, scores[0], most);
+        if (partial_of(g.first)) most = mask(g.first, scores[0]);
+        top = halves_max(most);
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) o[i] = f32x16(0.0f);
     }
-    for (uint32_t u = g.first; u < g.end; u += 2) {
-        step(u, std::integral_constant<int, 0>(), scores[0], scores[1]);
-        if (u + 1 < g.end) step(u + 1, std::integral_constant<int, 1>(), scores[1], scores[0]);
+    constexpr std::integral_constant<int, 0> k0{};
+    constexpr std::integral_constant<int, 1> k1{};
+    uint32_t u = g.first;
+    while (u < g.end) {
+        // up to here every row sees all keys of the units, which are of the table of unit u
+        const uint32_t full = in_prefix(u)
+                                  ? smaller(g.end, (uint32_t)a.prefix_len / kKeys)
+                                  : smaller(g.end, (kKind == kJoined ? g.prefix_units : 0u) + (uint32_t)own_first / kKeys);
+        for (; u + 4 <= full; u += 2) {
+            step(std::true_type(), u, k0, scores[0], scores[1]);
+            step(std::true_type(), u + 1, k1, scores[1], scores[0]);
+        }
+        step(std::false_type(), u, k0, scores[0], scores[1]);
+        if (u + 1 < g.end) step(std::false_type(), u + 1, k1, scores[1], scores[0]);
+        u += 2;
     }
 
     // ---- join the waves that split the keys, then write
-    auto finish = [&](int lane) {
+    auto finish = [&](int lane, bool whole, int64_t place) {
         const int half = lane >> 5;
         if constexpr (WK > 1) {
             if (half == 0) {
@@ -604,7 +707,7 @@ __device__ void segment(const AttendArgs& a, const Segment& g, const int32_t* cu
             sum = wk == 0 ? own + others : others + own;
             top = now;
             // piece i of the output is summed by the wave wk = i % WK
-            f32x4* const box = (f32x4*)smem;  // [row block, head_dim part][piece][4][lane]
+            f32x4* const box = (f32x4*)(smem + S::kStage);  // [row block, head_dim part][piece][4][lane]
             const int pair = wr + wd * WR;
 #pragma unroll
             for (int i = 0; i < kPieces; ++i) {
@@ -629,16 +732,17 @@ __device__ void segment(const AttendArgs& a, const Segment& g, const int32_t* cu
                     }
                 }
             }
+            lds_barrier();  // every wave has emptied its boxes
         }
         const bool nan = *poison_flag != 0;
-        const float by = nan ? NAN : whole ? 1.0f / sum : 1.0f;
+        const float by = nan ? forget(NAN) : whole ? 1.0f / sum : 1.0f;
         if (!whole && half == 0 && wk == 0 && wd == 0) {
             a.part_max[place + wr * 32 + lane] = top;
             a.part_sum[place + wr * 32 + lane] = sum;
         }
         // A lane has 16 values of its row; they go out by way of LDS, 8 lanes a row, in
         // whole lines of 128 bytes.
-        f32x4* const turn = (f32x4*)(smem + 2 * S::kTile + wave * 4096);  // (behind the box) [row][8], chunks flipped by row
+        f32x4* const turn = (f32x4*)(smem + S::kStage + wave * 4096);  // [row][8], chunks flipped by row
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
             if (i % WK != wk) continue;
@@ -668,48 +772,60 @@ __device__ void segment(const AttendArgs& a, const Segment& g, const int32_t* cu
     };
     sum = halves_sum(sum);
     top *= a.scale_log2;
-    if (poison) *poison_flag = 1;
+    if (work.poison) *poison_flag = 1;
+    const bool whole = kKind == kJoined && work.whole;
+    const int64_t place = work.place;
+    const bool more = work.advance();
     lds_barrier();  // every wave has done with the tiles
-    finish(forget(lane));
-    lds_barrier();  // LDS and the flag are free again
+    if (more) work.stage_first();  // (into the first two; what follows works in the others)
+    finish(forget(lane), whole, place);
+    lds_barrier();  // they and the flag are free again
     if (tid == 0) *poison_flag = 0;
+    return more;
 }
 
-// kPrefix and kOwn: waves that split the rows of the prefix's tasks and of the sequences' own.
-template <class T, int D, int kPrefix, int kOwn>
+template <class T, int D, int WR, Kind kKind>
+__device__ __forceinline__ void run(const AttendArgs& a, const Totals& t, const Deal& deal, const Batch& batch, uint32_t w,
+                                    char* smem, float (*wave_stats)[2][32], int* poison_flag, int* special_flag) {
+    if (w >= deal.groups) return;
+    Work<D, kKind> work{a, t, batch, (uint32_t)(uintptr_t)(SV_LDS char*)smem, w, group_start(deal, w + 1),
+                        {}, 0, false, group_start(deal, w), 0, 0, 0, false};
+    bool more = work.advance();
+    if (more) work.stage_first();
+    while (more) more = segment<T, D, WR>(work, smem, wave_stats, poison_flag, special_flag);
+}
+
+// kPrefix and kRows: waves that split the rows of the prefix's tasks (0: there are
+// none, a sequence's tasks begin with it) and of the sequences' own.
+template <class T, int D, int kPrefix, int kRows>
 __global__ void __launch_bounds__(kThreads, (D > 128 ? 1 : 2)) attend_kernel(AttendArgs a) {
     extern __shared__ __attribute__((aligned(16))) char smem[];
     __shared__ uint32_t wave_sums[4][2];
     __shared__ float wave_stats[4][2][32];
-    __shared__ int poison_flag;
+    __shared__ int poison_flag, special_flag;
     const Split& split = a.split;
     int32_t* const words = (int32_t*)(smem + 2 * Shape<D>::kStage);
     const Batch batch{words, (uint32_t*)words + split.batch + 1, words + 2 * (split.batch + 1)};
-    if (threadIdx.x == 0) poison_flag = 0;
+    if (threadIdx.x == 0) poison_flag = special_flag = 0;
     const Totals t = sum_batch(split, batch, wave_sums);
     if (blockIdx.x == 0)  // for the kernel that joins the parts
         for (int b = threadIdx.x; b <= split.batch; b += kThreads) {
             a.cum_tokens[b] = batch.cum_tokens[b];
             a.cum_cost[b] = batch.cum_cost[b];
         }
-    if (blockIdx.x >= t.groups) return;
-    // Workgroups go round the 8 XCDs; those of one XCD take adjoining runs, so
-    // that the tasks that share keys read them through one L2.
-    const uint32_t w = (t.groups % 8 == 0) ? (blockIdx.x % 8) * (t.groups / 8) + blockIdx.x / 8 : blockIdx.x;
-    const uint32_t end = group_start(t, w + 1);
-    for (uint32_t u = group_start(t, w); u < end;) {
-        Segment g = task_at(split, t, batch.cum_cost, u, [&](int32_t b) { return sequence(batch, b); });
-        cut(g, u, end);
-        if (g.first == g.end) break;  // (the run ends within the task's cost of starting)
-        const bool whole = whole_task(split, g);
-        const int64_t place = part_place(split, g, w);
-        u = g.task_start + g.end;
-        g.first += g.offset;  // (from here on: units of the keys)
-        g.end += g.offset;
-        if (kPrefix == kOwn || g.b >= 0)
-            segment<T, D, kOwn>(a, g, batch.cum_tokens, smem, wave_stats, &poison_flag, whole, place);
-        else
-            segment<T, D, kPrefix>(a, g, batch.cum_tokens, smem, wave_stats, &poison_flag, whole, place);
+    // Workgroups go round the 8 XCDs.  Those of one XCD take adjoining runs of the
+    // tasks that share keys, to read them through one L2.
+    const uint32_t xcd = blockIdx.x % 8, place = blockIdx.x / 8;
+    if constexpr (kPrefix == 0) {
+        const uint32_t w = t.own.groups % 8 == 0 ? xcd * (t.own.groups / 8) + place : blockIdx.x;
+        if (blockIdx.x < t.own.groups)
+            run<T, D, kRows, kJoined>(a, t, t.own, batch, w, smem, wave_stats, &poison_flag, &special_flag);
+    } else if (blockIdx.x < t.prefix_places) {
+        const uint32_t w = t.prefix.groups == t.prefix_places ? xcd * (t.prefix_places / 8) + place : blockIdx.x;
+        run<T, D, kPrefix, kShared>(a, t, t.prefix, batch, w, smem, wave_stats, &poison_flag, &special_flag);
+    } else {
+        run<T, D, kRows, kOwn>(a, t, t.own, batch, blockIdx.x - t.prefix_places, smem, wave_stats, &poison_flag,
+                               &special_flag);
     }
 }
 
@@ -810,9 +926,8 @@ __global__ void __launch_bounds__(kThreads) attend_join_tasks_kernel(AttendArgs 
     const Split& split = a.split;
     const Totals t = totals(split, uniform(a.cum_tokens[split.batch]), uniform(a.cum_cost[split.batch]));
     const uint32_t w = blockIdx.x + 1;
-    if (w >= t.groups) return;
-    const Segment g =
-        task_at(split, t, a.cum_cost, group_start(t, w), [&](int32_t b) { return sequence(split, b); });
+    if (w >= t.own.groups) return;
+    const Segment g = own_task_at(split, a.cum_cost, group_start(t.own, w), [&](int32_t b) { return sequence(split, b); });
     uint32_t w0, w1;
     if (!first_border(t, g, w, w0, w1)) return;
     const int wave = uniform((int32_t)(threadIdx.x >> 6));
@@ -835,15 +950,18 @@ template <class T, int D>
 sv_status_t launch(const AttendArgs& a, hipStream_t stream) {
     const size_t lds = 2 * Shape<D>::kStage + 3 * sizeof(int32_t) * ((size_t)a.split.batch + 1);
     const uint32_t groups = (uint32_t)a.split.plan.groups;
-    const int own = a.split.plan.own_rows / 32, prefix = a.split.plan.joined ? own : a.split.plan.prefix_rows / 32;
-    auto go = [&](auto p, auto o) {
-        hipLaunchKernelGGL((attend_kernel<T, D, decltype(p)::value, decltype(o)::value>), dim3(groups), dim3(kThreads),
-                           lds, stream, a);
+    auto go = [&](auto prefix, auto own) {
+        hipLaunchKernelGGL((attend_kernel<T, D, decltype(prefix)::value, decltype(own)::value>), dim3(groups),
+                           dim3(kThreads), lds, stream, a);
     };
+    constexpr std::integral_constant<int, 0> k0{};
     constexpr std::integral_constant<int, 1> k1{};
     constexpr std::integral_constant<int, 2> k2{};
     constexpr std::integral_constant<int, kMaxTaskRows<D> / 32> k4{};
-    if (prefix == 1)
+    const int own = a.split.plan.own_rows / 32, prefix = a.split.plan.joined ? 0 : a.split.plan.prefix_rows / 32;
+    if (prefix == 0)
+        own == 1 ? go(k0, k1) : own == 2 ? go(k0, k2) : go(k0, k4);
+    else if (prefix == 1)
         go(k1, k1);
     else if (prefix == 2)
         own == 1 ? go(k2, k1) : go(k2, k2);

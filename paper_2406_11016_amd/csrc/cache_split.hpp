@@ -67,48 +67,59 @@ constexpr uint32_t tile_cost(const Split& a, const Sequence& s, int32_t rt) {
     return n == 0 ? 0 : n + kTaskUnits;
 }
 
-// The tasks in order: the shared prefix's, then each sequence's own (sequence, head,
-// row tile).  The prefix is cut into chunks of a workgroup's share of all units,
-// and its tasks are ordered by key/value head, chunk, row tile: workgroups next to
-// each other then run over the same keys at the same time, for other rows, and
-// find them in their XCD's L2.  (With tasks over the whole prefix every workgroup
-// was somewhere else in it: 18,432 rows and 16,384 keys read 1.07 GB from behind
-// the L2s at 5.8 TB/s, which took 183 us, whatever was computed.)
+// A cost dealt to workgroups in equal runs; the first `longer` have one more.
+struct Deal {
+    uint32_t cost, groups, each, longer;
+};
+constexpr Deal deal(uint32_t cost, uint32_t groups) {
+    Deal d{cost, smaller(groups, cost), 0, 0};
+    if (d.groups == 0) return d;
+    d.each = cost / d.groups;
+    d.longer = cost - d.each * d.groups;
+    return d;
+}
+// Workgroup w's run begins at group_start(w); group_of is its inverse.
+constexpr uint32_t group_start(const Deal& d, uint32_t w) { return w * d.each + smaller(w, d.longer); }
+constexpr uint32_t group_of(const Deal& d, uint32_t u) {
+    const uint32_t border = d.longer * (d.each + 1);
+    return u < border ? u / (d.each + 1) : d.longer + (u - border) / d.each;
+}
+
+// The tasks: the shared prefix's, and each sequence's own in the order of sequence,
+// head, row tile.  Each kind has workgroups of its own, by its cost, in every XCD: the
+// prefix's wait for the matrix units and the others for memory, so a CU has some of
+// both.
+//
+// The prefix is cut into chunks of about a workgroup's share, and its tasks are
+// ordered by key/value head, chunk, row tile: workgroups next to each other then run
+// over the same keys at the same time, for other rows, and find them in their XCD's
+// L2.  (With tasks over the whole prefix every workgroup was somewhere else in it:
+// 18,432 rows and 16,384 keys read 1.07 GB from behind the L2s, and 0.40 GB so.)
 struct Totals {
     int32_t tokens, prefix_tiles;  // prefix tiles of one key/value head
-    uint32_t prefix_cost, cost;    // cost of all prefix tasks; of all tasks
-    uint32_t groups;               // workgroups that take part
-    uint32_t each, longer;         // cost dealt to a workgroup; the first `longer` have one more
     uint32_t chunk, chunks;        // units of a chunk of the prefix; chunks
+    Deal prefix, own;
+    uint32_t prefix_places;        // workgroups of the grid that are the prefix's, a multiple of 8
 };
 constexpr Totals totals(const Split& a, int32_t tokens, uint32_t own_cost) {
     Totals t{};
     t.tokens = tokens;
-    if (!a.plan.joined)
+    const uint32_t groups = (uint32_t)a.plan.groups;
+    if (!a.plan.joined && tokens > 0) {
         t.prefix_tiles =
             (int32_t)(((uint32_t)tokens * (uint32_t)a.group + (uint32_t)a.plan.prefix_rows - 1) >> a.plan.prefix_shift);
-    const uint32_t rows_heads = (uint32_t)t.prefix_tiles * (uint32_t)a.kv_heads, units = (uint32_t)a.prefix_units;
-    t.cost = rows_heads * (units + kTaskUnits) + own_cost;
-    t.groups = smaller((uint32_t)a.plan.groups, t.cost);
-    if (t.groups == 0) return t;
-    if (rows_heads != 0) {
-        const uint32_t share = t.cost / t.groups;
+        const uint32_t tasks = (uint32_t)t.prefix_tiles * (uint32_t)a.kv_heads, units = (uint32_t)a.prefix_units;
+        const uint32_t cost = tasks * (units + kTaskUnits);
+        const uint32_t eighths =
+            (uint32_t)(((uint64_t)(groups / 8) * cost + (cost + own_cost) / 2) / ((uint64_t)cost + own_cost));
+        t.prefix_places = 8 * (eighths < 1 ? 1u : smaller(eighths, groups / 8 - 1));
+        const uint32_t share = cost / smaller(t.prefix_places, cost);
         t.chunk = share > 2 * kTaskUnits ? share - kTaskUnits : 1 + share / 2;
         t.chunks = (units + t.chunk - 1) / t.chunk;
-        t.prefix_cost = rows_heads * (units + t.chunks * kTaskUnits);
-        t.cost = t.prefix_cost + own_cost;
-        t.groups = smaller((uint32_t)a.plan.groups, t.cost);
+        t.prefix = deal(tasks * (units + t.chunks * kTaskUnits), t.prefix_places);
     }
-    t.each = t.cost / t.groups;
-    t.longer = t.cost - t.each * t.groups;
+    t.own = deal(own_cost, groups - t.prefix_places);
     return t;
-}
-
-// Workgroup w's run of the cost begins at group_start(w); group_of is its inverse.
-constexpr uint32_t group_start(const Totals& t, uint32_t w) { return w * t.each + smaller(w, t.longer); }
-constexpr uint32_t group_of(const Totals& t, uint32_t u) {
-    const uint32_t border = t.longer * (t.each + 1);
-    return u < border ? u / (t.each + 1) : t.longer + (u - border) / t.each;
 }
 
 // The last b of n with cum[b] <= x (cum[0] <= x < cum[n]).
@@ -128,7 +139,7 @@ constexpr int32_t find(const I* cum, int32_t n, I x) {
 // A run of units of one task.
 struct Segment {
     uint32_t task;               // number among the prefix's, or among the sequences' own tasks
-    uint32_t task_start, units;  // where its units begin in the cost of all tasks (behind kTaskUnits); its units
+    uint32_t task_start, units;  // where its units begin in its kind's cost (behind kTaskUnits); its units
     uint32_t first, end;         // this run, within the task
     uint32_t offset;             // units of the prefix before the task's chunk
     uint32_t prefix_units;       // units of the prefix that the task begins with
@@ -137,37 +148,38 @@ struct Segment {
     bool bad;
 };
 
-// The task at place u of the cost.  `sequence_of(b)` gives sequence b;
-// `find_tile(sequence, at, start)` the row tile that holds place `at` of a sequence
+// The prefix's task at place u of its cost.
+constexpr Segment prefix_task(const Split& a, const Totals& t, uint32_t u) {
+    Segment g{};
+    const uint32_t tiles = (uint32_t)t.prefix_tiles, units = (uint32_t)a.prefix_units;
+    const uint32_t head = tiles * (units + t.chunks * kTaskUnits), chunk_cost = (t.chunk + kTaskUnits) * tiles;
+    g.kv_head = (int32_t)(u / head);
+    const uint32_t at = u - (uint32_t)g.kv_head * head, chunk = at / chunk_cost, in_chunk = at - chunk * chunk_cost;
+    g.offset = chunk * t.chunk;
+    g.units = smaller(t.chunk, units - g.offset);
+    const uint32_t tile = in_chunk / (g.units + kTaskUnits);
+    g.task = ((uint32_t)g.kv_head * t.chunks + chunk) * tiles + tile;
+    g.task_start = u - (in_chunk - tile * (g.units + kTaskUnits)) + kTaskUnits;
+    g.prefix_units = units;
+    g.row0 = (int32_t)tile << a.plan.prefix_shift;
+    g.b = -1;
+    return g;
+}
+// The sequences' own task at place u of their cost.  `sequence_of(b)` gives sequence
+// b; `find_tile(sequence, at, start)` the row tile that holds place `at` of a sequence
 // and head, and the place at which that tile's task begins.
 template <class SequenceOf, class FindTile>
-constexpr Segment locate(const Split& a, const Totals& t, const uint32_t* cum_cost, uint32_t u, SequenceOf sequence_of,
-                         FindTile find_tile) {
+constexpr Segment own_task(const Split& a, const uint32_t* cum_cost, uint32_t u, SequenceOf sequence_of,
+                           FindTile find_tile) {
     Segment g{};
-    if (u < t.prefix_cost) {
-        const uint32_t tiles = (uint32_t)t.prefix_tiles, units = (uint32_t)a.prefix_units;
-        const uint32_t head = tiles * (units + t.chunks * kTaskUnits), chunk_cost = (t.chunk + kTaskUnits) * tiles;
-        g.kv_head = (int32_t)(u / head);
-        const uint32_t at = u - (uint32_t)g.kv_head * head, chunk = at / chunk_cost, in_chunk = at - chunk * chunk_cost;
-        g.offset = chunk * t.chunk;
-        g.units = smaller(t.chunk, units - g.offset);
-        const uint32_t tile = in_chunk / (g.units + kTaskUnits);
-        g.task = ((uint32_t)g.kv_head * t.chunks + chunk) * tiles + tile;
-        g.task_start = u - (in_chunk - tile * (g.units + kTaskUnits)) + kTaskUnits;
-        g.prefix_units = units;
-        g.row0 = (int32_t)tile << a.plan.prefix_shift;
-        g.b = -1;
-        return g;
-    }
-    const uint32_t v = u - t.prefix_cost;
-    g.b = find(cum_cost, a.batch, v);
+    g.b = find(cum_cost, a.batch, u);
     const Sequence s = sequence_of(g.b);
     const uint32_t base = cum_cost[g.b], head = (cum_cost[g.b + 1] - base) / (uint32_t)a.kv_heads;
-    g.kv_head = (int32_t)((v - base) / head);
+    g.kv_head = (int32_t)((u - base) / head);
     uint32_t start = 0;
-    const int32_t rt = find_tile(s, v - base - (uint32_t)g.kv_head * head, start);
+    const int32_t rt = find_tile(s, u - base - (uint32_t)g.kv_head * head, start);
     g.task = (uint32_t)(g.b * a.kv_heads + g.kv_head) * (uint32_t)a.plan.own_tiles + (uint32_t)rt;
-    g.task_start = t.prefix_cost + base + (uint32_t)g.kv_head * head + start + kTaskUnits;
+    g.task_start = base + (uint32_t)g.kv_head * head + start + kTaskUnits;
     g.units = tile_units(a, s, rt);
     g.prefix_units = a.plan.joined ? (uint32_t)a.prefix_units : 0u;
     g.row0 = rt << a.plan.own_shift;
@@ -176,8 +188,8 @@ constexpr Segment locate(const Split& a, const Totals& t, const uint32_t* cum_co
     g.bad = s.bad;
     return g;
 }
-// A workgroup's run of the task that it finds at place u of the cost, its own run
-// ending before place `end`; empty (first == end) if it ends before the task's units.
+// A workgroup's run of the task that it finds at place u of the cost, its run of the
+// cost ending before place `end`; empty (first == end) if it ends before the task's units.
 constexpr void cut(Segment& g, uint32_t u, uint32_t end) {
     g.first = u > g.task_start ? u - g.task_start : 0u;
     g.end = end > g.task_start ? smaller(g.units, end - g.task_start) : 0u;
@@ -196,8 +208,8 @@ constexpr int32_t own_end(const Split& a, const Segment& g) {
 }
 
 // Row place of a segment's part.  With a shared prefix every segment of every task
-// has one: segments in order differ in their task or in their workgroup, and so in
-// the sum of the two.  Without one only cut tasks have parts: a workgroup cuts at
+// has one: segments of a kind in order differ in their task or in their workgroup,
+// and so in the sum of the two.  Without one only cut tasks have parts: a workgroup cuts at
 // most the one that it begins in and the one that it ends in.
 constexpr bool whole_task(const Split& a, const Segment& g) {
     return a.plan.joined && g.first == 0 && g.end == g.units;
@@ -219,8 +231,8 @@ constexpr int64_t prefix_part(const Split& a, const Totals& t, int32_t kv_head, 
     const uint32_t start = (uint32_t)kv_head * tiles * ((uint32_t)a.prefix_units + t.chunks * kTaskUnits) +
                            chunk * (t.chunk + kTaskUnits) * tiles + tile * (units + kTaskUnits) + kTaskUnits;
     const uint32_t task = ((uint32_t)kv_head * t.chunks + chunk) * tiles + tile;
-    const uint32_t w = group_of(t, start) + (k - chunk * kChunkParts);
-    if (w > group_of(t, start + units - 1)) return -1;
+    const uint32_t w = group_of(t.prefix, start) + (k - chunk * kChunkParts);
+    if (w > group_of(t.prefix, start + units - 1)) return -1;
     return (int64_t)(task + w) * a.plan.prefix_rows + (r & (a.plan.prefix_rows - 1));
 }
 
@@ -233,10 +245,10 @@ struct Parts {
 constexpr Parts own_parts(const Split& a, const Totals& t, const Sequence& s, uint32_t cost_before, uint32_t cost,
                           int32_t b, int32_t token, int32_t kv_head, int32_t g) {
     const int32_t r = token * a.group + g, tile = r >> a.plan.own_shift;
-    uint32_t start = t.prefix_cost + cost_before + (uint32_t)kv_head * (cost / (uint32_t)a.kv_heads) + kTaskUnits;
+    uint32_t start = cost_before + (uint32_t)kv_head * (cost / (uint32_t)a.kv_heads) + kTaskUnits;
     for (int32_t rt = 0; rt < tile; ++rt) start += tile_cost(a, s, rt);
     const uint32_t task = (uint32_t)(b * a.kv_heads + kv_head) * (uint32_t)a.plan.own_tiles + (uint32_t)tile;
-    const uint32_t w0 = group_of(t, start), w1 = group_of(t, start + tile_units(a, s, tile) - 1);
+    const uint32_t w0 = group_of(t.own, start), w1 = group_of(t.own, start + tile_units(a, s, tile) - 1);
     return Parts{a.plan.own_parts + (int64_t)(task + w0) * a.plan.own_rows + (r - (tile << a.plan.own_shift)),
                  a.plan.own_rows, (int32_t)(w1 - w0) + 1};
 }
@@ -244,9 +256,9 @@ constexpr Parts own_parts(const Split& a, const Totals& t, const Sequence& s, ui
 // Without one: whether the border before workgroup w (w > 0) is the first to cut a
 // task's units, and then the workgroups that have parts of it.
 constexpr bool first_border(const Totals& t, const Segment& g, uint32_t w, uint32_t& w0, uint32_t& w1) {
-    w0 = group_of(t, g.task_start);
-    w1 = group_of(t, g.task_start + g.units - 1);
-    return group_start(t, w) > g.task_start && w == w0 + 1;
+    w0 = group_of(t.own, g.task_start);
+    w1 = group_of(t.own, g.task_start + g.units - 1);
+    return group_start(t.own, w) > g.task_start && w == w0 + 1;
 }
 // Row r of a task cut by the borders of workgroups w0 .. w1; the
 // first one's part is its last segment's, the others' are their first ones'.

@@ -88,18 +88,27 @@ static void simulate(const Case& c, int id) {
     std::map<std::pair<bool, uint32_t>, std::vector<Got>> got;
     std::map<std::pair<bool, uint32_t>, Segment> tasks;
     std::vector<std::pair<int64_t, int64_t>> places;
-    uint32_t covered = 0;
     std::map<std::pair<bool, uint32_t>, uint32_t> done;  // units of each task
-    for (uint32_t w = 0; w < t.groups; ++w) {
-        const uint32_t end = group_start(t, w + 1);
-        uint32_t u = group_start(t, w);
+    CHECK(t.prefix_places % 8 == 0 && t.prefix.groups <= t.prefix_places, "case %d", id);
+    CHECK(t.prefix_places + t.own.groups <= (uint32_t)plan.groups, "case %d", id);
+    CHECK((t.prefix.cost == 0) == (plan.joined || t.tokens == 0), "case %d", id);
+    for (const bool shared : {true, false}) {
+    const Deal& d = shared ? t.prefix : t.own;
+    uint32_t covered = 0;
+    for (uint32_t w = 0; w < d.groups; ++w) {
+        const uint32_t end = group_start(d, w + 1);
+        uint32_t u = group_start(d, w);
         CHECK(u == covered && u < end, "case %d: group %u", id, w);
         covered = end;
         while (u < end) {
-            CHECK(group_of(t, u) == w, "case %d: unit %u", id, u);
-            Segment g = locate(
-                a, t, cum_cost.data(), u, [&](int32_t b) { return sequence(a, b); },
-                [&](const Sequence& s, uint32_t at, uint32_t& start) { return find_tile_host(a, s, at, start); });
+            CHECK(group_of(d, u) == w, "case %d: unit %u", id, u);
+            Segment g = shared ? prefix_task(a, t, u)
+                               : own_task(
+                                     a, cum_cost.data(), u, [&](int32_t b) { return sequence(a, b); },
+                                     [&](const Sequence& s, uint32_t at, uint32_t& start) {
+                                         return find_tile_host(a, s, at, start);
+                                     });
+            CHECK((g.b < 0) == shared, "case %d", id);
             CHECK(u + kTaskUnits >= g.task_start && u < g.task_start + g.units && g.units > 0, "case %d: unit %u", id, u);
             cut(g, u, end);
             if (g.first == g.end) break;
@@ -131,7 +140,8 @@ static void simulate(const Case& c, int id) {
             u = g.task_start + g.end;
         }
     }
-    CHECK(covered == t.cost, "case %d", id);
+    CHECK(covered == d.cost, "case %d", id);
+    }
     for (const auto& x : tasks) CHECK(done[x.first] == x.second.units, "case %d: a task not done", id);
     std::sort(places.begin(), places.end());
     for (size_t i = 1; i < places.size(); ++i) CHECK(places[i - 1].second <= places[i].first, "case %d", id);
@@ -183,19 +193,19 @@ static void simulate(const Case& c, int id) {
                     } else if (got.count({false, task})) {
                         const auto& have = got[std::make_pair(false, task)];
                         uint32_t w0 = 0, w1 = 0;
-                        CHECK(first_border(t, g, group_of(t, g.task_start) + 1, w0, w1), "case %d", id);
+                        CHECK(first_border(t, g, group_of(t.own, g.task_start) + 1, w0, w1), "case %d", id);
                         CHECK(w1 > w0 && have.size() == w1 - w0 + 1, "case %d", id);
                         same(first_cut_part(a, w0, r % plan.own_rows), have, 0, r % plan.own_rows);
                         same(later_cut_parts(a, w0, w1, r % plan.own_rows), have, 1, r % plan.own_rows);
                         // one workgroup of the joining kernel takes it
-                        for (uint32_t w = 1; w < t.groups && r % plan.own_rows == 0; ++w) {
-                            const uint32_t u = group_start(t, w);
+                        for (uint32_t w = 1; w < t.own.groups && r % plan.own_rows == 0; ++w) {
+                            const uint32_t u = group_start(t.own, w);
                             if (u + kTaskUnits < g.task_start || u >= g.task_start + g.units) continue;
                             uint32_t x0, x1;
                             CHECK(first_border(t, g, w, x0, x1) == (w == w0 + 1), "case %d", id);
                         }
                     } else {
-                        CHECK(group_of(t, g.task_start) == group_of(t, g.task_start + g.units - 1), "case %d", id);
+                        CHECK(group_of(t.own, g.task_start) == group_of(t.own, g.task_start + g.units - 1), "case %d", id);
                     }
                 }
     }
