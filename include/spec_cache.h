@@ -48,6 +48,7 @@ extern "C" {
 
 /* Largest batch of one call. */
 #define SV_CACHE_MAX_BATCH 4096
+#define SV_CACHE_MAX_BATCH_D256 2048  /* spec_cache_attend at head_dim 256 (the batch's sums share the LDS) */
 
 /*
  * The tables of a batch.  num_pages is the number of pages of the caches;
@@ -130,7 +131,8 @@ sv_status_t spec_cache_append(const sv_cache_append_desc_t* desc, hipStream_t st
  *   out[b, i, h] = sum_j w_j v_j / sum_j w_j,   w_j = exp(scale q[b, i, h] . k_j)
  *
  * with the keys and values of head h / (q_heads / kv_heads).  The shared prefix
- * is read once for the batch.  q and out [batch, max_new, q_heads, head_dim];
+ * is read once for the batch.  q and out [batch, max_new, q_heads, head_dim] do
+ * not overlap;
  * rows behind counts[b] are neither read nor written (all of them where
  * counts[b] <= 0; without `counts` every sequence has max_new).  Entries of the
  * cache that a token does not see have no influence on it, whatever their bits.
@@ -143,8 +145,8 @@ sv_status_t spec_cache_append(const sv_cache_append_desc_t* desc, hipStream_t st
  * of every sequence), lengths[b] < 0, counts[b] > max_new, or lengths[b] +
  * counts[b] > max_pages * page_size.
  *
- * head_dim is 64, 80, 96, 128 or 256; q_heads a multiple of kv_heads; scale
- * finite and > 0.  Pointers are aligned to 16 bytes, strides (elements; batch,
+ * head_dim is 64, 80, 96, 128 or 256 (for at most SV_CACHE_MAX_BATCH_D256
+ * sequences); q_heads a multiple of kv_heads; scale between 1e-30 and 1e30.  Pointers are aligned to 16 bytes, strides (elements; batch,
  * token, head) are multiples of 8.  `workspace` holds
  * spec_cache_attend_workspace_bytes() bytes, aligned to 16, and needs no
  * initialisation.

@@ -59,7 +59,7 @@ constexpr int kAttendKeys = 64;
 // many units more where work is dealt out.
 constexpr uint32_t kTaskUnits = 3;
 
-// How a call's work is cut (see cache_attend.hip).
+// How a call's work is cut (see cache_attend.hpp).
 struct AttendPlan {
     // joined: a task runs over the prefix and then over its sequence's keys, and
     // only tasks cut by a workgroup's border have parts.  Otherwise the prefix
@@ -72,6 +72,8 @@ struct AttendPlan {
     int64_t own_parts, rows;      // row places of the parts: of the first own one, of all
     size_t cum_bytes;             // one array of sums over the batch
 };
+
+constexpr size_t kTotalsBytes = 256;  // room in the workspace for the split's totals, see cache_split.hpp
 
 inline bool head_dim_ok(int32_t d) { return d == 64 || d == 80 || d == 96 || d == 128 || d == 256; }
 
@@ -113,6 +115,7 @@ inline AttendPlan attend_plan(int32_t batch, int32_t max_new, int32_t q_heads, i
 inline bool attend_sizes_ok(int32_t batch, int32_t max_new, int32_t q_heads, int32_t kv_heads, int32_t head_dim) {
     return batch >= 1 && batch <= SV_CACHE_MAX_BATCH && max_new >= 1 && kv_heads >= 1 && q_heads >= kv_heads &&
            q_heads <= 65536 && q_heads % kv_heads == 0 && head_dim_ok(head_dim) &&
+           (head_dim <= 128 || batch <= SV_CACHE_MAX_BATCH_D256) &&
            (int64_t)batch * max_new <= INT_MAX && (int64_t)batch * max_new * q_heads <= INT_MAX;
 }
 
@@ -133,7 +136,7 @@ inline size_t attend_workspace_bytes(int32_t batch, int32_t max_new, int32_t q_h
     size_t most = 0;
     for (const bool prefix : {false, true}) {
         const AttendPlan p = attend_plan(batch, max_new, q_heads, kv_heads, head_dim, prefix);
-        const size_t n = 2 * p.cum_bytes + (size_t)p.rows * ((size_t)head_dim + 2) * sizeof(float);
+        const size_t n = 2 * p.cum_bytes + kTotalsBytes + (size_t)p.rows * ((size_t)head_dim + 2) * sizeof(float);
         if (n > most) most = n;
     }
     return (most + 255) / 256 * 256;

@@ -71,7 +71,7 @@ static void simulate(const Case& c, int id) {
     const AttendPlan plan = attend_plan(c.batch, c.max_new, c.q_heads, c.kv_heads, c.head_dim, c.prefix_len > 0);
     CHECK(attend_units_ok(d, plan), "case %d", id);
     const size_t bytes = attend_workspace_bytes(c.batch, c.max_new, c.q_heads, c.kv_heads, c.head_dim);
-    CHECK(2 * plan.cum_bytes + (size_t)plan.rows * (c.head_dim + 2) * 4 <= bytes, "case %d", id);
+    CHECK(sizeof(Totals) <= kTotalsBytes && 2 * plan.cum_bytes + kTotalsBytes + (size_t)plan.rows * (c.head_dim + 2) * 4 <= bytes, "case %d", id);
     CHECK(plan.cum_bytes % 16 == 0 && plan.rows % 4 == 0, "case %d", id);  // the parts lie on 16 bytes
     const Split a = make_split(d, plan);
     std::vector<int32_t> cum_tokens(c.batch + 1, 0);
@@ -292,6 +292,8 @@ static void section_arguments() {
     BAD(SV_ERR_DTYPE, d.dtype = (sv_dtype_t)9);
     BAD(SV_ERR_SHAPE, d.batch = 0);
     BAD(SV_ERR_SHAPE, d.batch = SV_CACHE_MAX_BATCH + 1);
+    BAD(SV_ERR_SHAPE, d.head_dim = 256; d.page_stride = 2 * 16 * 256; d.batch = SV_CACHE_MAX_BATCH_D256 + 1);
+    BAD(SV_ERR_WORKSPACE, d.head_dim = 256; d.page_stride = 2 * 16 * 256; d.batch = SV_CACHE_MAX_BATCH_D256);
     BAD(SV_ERR_SHAPE, d.max_new = 0);
     BAD(SV_ERR_SHAPE, d.max_new = 1 << 30);
     BAD(SV_ERR_SHAPE, d.kv_heads = 0);
@@ -325,7 +327,9 @@ static void section_arguments() {
 #undef BAD
     CHECK(attend_workspace_bytes(0, 1, 1, 1, 64) == 0 && attend_workspace_bytes(1, 0, 1, 1, 64) == 0 &&
               attend_workspace_bytes(1, 1, 3, 2, 64) == 0 && attend_workspace_bytes(1, 1, 1, 1, 65) == 0 &&
-              attend_workspace_bytes(1, 1, 1, 0, 64) == 0,
+              attend_workspace_bytes(1, 1, 1, 0, 64) == 0 &&
+              attend_workspace_bytes(SV_CACHE_MAX_BATCH_D256 + 1, 1, 1, 1, 256) == 0 &&
+              attend_workspace_bytes(SV_CACHE_MAX_BATCH, 1, 1, 1, 128) != 0,
           "sizes");
     // the counts of units stay below 2^31, or the call is refused
     sv_cache_attend_desc_t d = good();

@@ -7,6 +7,7 @@ import pytest
 import torch
 
 from paper_2406_11016_amd import paged_cache
+from paper_2406_11016_amd.binding import SpecVerifyError
 from paper_2406_11016_amd.paged_cache import PagedCache
 from tests.cache_util import TORCH_DTYPES, attend_bound, attend_reference
 
@@ -133,6 +134,17 @@ def test_many_sequences(prefix):
     B = 4096
     x = make(B, 1, 1, 1, 64, 16, prefix, [b % 17 for b in range(B)], [b % 2 for b in range(B)], "f16", seed=5)
     check(x, prefix, "f16")
+
+
+@pytest.mark.parametrize("prefix", [0, 40])
+@pytest.mark.parametrize("B,D", [(4096, 128), (2048, 256)])
+def test_largest_batches(B, D, prefix):
+    """The batch's sums take the most LDS beside the tiles."""
+    x = make(B, 1, 1, 1, D, 16, prefix, [b % 13 for b in range(B)], [b % 3 - 1 for b in range(B)], "bf16", seed=6)
+    check(x, prefix, "bf16")
+    if D == 256:
+        with pytest.raises(SpecVerifyError, match="invalid sizes"):
+            paged_cache.new_attend_workspace(B + 1, 1, 1, 1, D, "cuda")
 
 
 def test_nothing_to_do():
