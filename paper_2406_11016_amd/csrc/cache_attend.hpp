@@ -962,6 +962,42 @@ __global__ void __launch_bounds__(kThreads) attend_join_rows_kernel(AttendArgs a
 // takes kJoinRows of its rows.  (Of 32,768 rows in two parts each, and of 65,408: 12.9
 // and 31.2 us with 16 rows a block, 13.9 and 34.5 with 8, 16.1 and 32.1 with 32.)
 constexpr int kJoinRows = 16;
+
+// The same from two parts each, which is what there is where tasks are many: a team of
+// D / 4 lanes a row, and all rows' loads under way at a time.
+template <class T, int D, class RowOut>
+__device__ __forceinline__ void join_two(const AttendArgs& a, int64_t first, int64_t second, int r0, RowOut row_out) {
+    constexpr int kLanes = D / 4, kTeams = 64 / kLanes * (kThreads / 64), kEach = (kJoinRows + kTeams - 1) / kTeams;
+    const int lane = threadIdx.x & 63, team = (int)(threadIdx.x >> 6) * (64 / kLanes) + lane / kLanes;
+    const int d = (lane % kLanes) * 4;
+    if (lane / kLanes >= 64 / kLanes) return;
+    uint16_t* to[kEach];
+    float most[kEach][2], sum[kEach][2];
+    f32x4 x[kEach][2];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int r = i * kTeams + team;
+        to[i] = r < kJoinRows ? row_out(r0 + r) : nullptr;
+        if (to[i] == nullptr) continue;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int64_t at = (k == 0 ? first : second) + r0 + r;
+            most[i][k] = a.part_max[at];
+            sum[i][k] = a.part_sum[at];
+            x[i][k] = *(const f32x4*)(a.part_out + at * D + d);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        if (to[i] == nullptr) continue;
+        const float top = fmaxf(most[i][0], most[i][1]), ref = top == -INFINITY ? 0.0f : top;
+        const float w0 = exp2_hw(most[i][0] - ref), w1 = exp2_hw(most[i][1] - ref);
+        f32x4 all = w0 * x[i][0];
+        all += w1 * x[i][1];
+        all *= 1.0f / (w0 * sum[i][0] + w1 * sum[i][1]);
+        *(u32x2*)(to[i] + d) = __builtin_bit_cast(u32x2, __builtin_convertvector(all, typename T::V4));
+    }
+}
 template <class T, int D>
 __global__ void __launch_bounds__(kThreads) attend_join_tasks_kernel(AttendArgs a) {
     const Split& split = a.split;
@@ -973,18 +1009,27 @@ __global__ void __launch_bounds__(kThreads) attend_join_tasks_kernel(AttendArgs 
     if (!first_border(t, g, w, w0, w1)) return;
     const int n = 1 + (int)(w1 - w0), end = (int)(blockIdx.y + 1) * kJoinRows;
     int r = (int)blockIdx.y * kJoinRows + uniform((int32_t)(threadIdx.x >> 6));
+    auto row_out = [&](int of) -> uint16_t* {
+        const int row = g.row0 + of, token = row / split.group;
+        const int head = g.kv_head * split.group + (row - token * split.group);
+        return token < g.count ? a.out + g.b * a.out_stride[0] + token * a.out_stride[1] + head * a.out_stride[2] : nullptr;
+    };
+    if (n == 2) {
+        join_two<T, D>(a, first_cut_part(split, w0, 0).first, later_cut_parts(split, w0, w1, 0).first, (int)blockIdx.y * kJoinRows,
+                       row_out);
+        return;
+    }
     auto place = [&](int k) {
         const Parts first = first_cut_part(split, w0, r), later = later_cut_parts(split, w0, w1, r);
         return k == 0 ? first.first : later.first + (k - 1) * later.step;
     };
 #pragma unroll 1
     for (; r < end; r += kThreads / 64) {
-        const int row = g.row0 + r, token = row / split.group;
-        const int head = g.kv_head * split.group + (row - token * split.group);
-        if (token >= g.count) return;
+        uint16_t* const to = row_out(r);
+        if (to == nullptr) return;
         Joiner<D> parts(a);
         parts.fetch(0, n, place);
-        parts.template join<T>(n, place, a.out + g.b * a.out_stride[0] + token * a.out_stride[1] + head * a.out_stride[2]);
+        parts.template join<T>(n, place, to);
     }
 }
 

@@ -104,7 +104,7 @@ inline AttendPlan attend_plan(int32_t batch, int32_t max_new, int32_t q_heads, i
         p.rows = 2 * (int64_t)p.groups * p.own_rows;
     } else {
         const int64_t prefix_tasks = kv_heads * ((batch * rows + p.prefix_rows - 1) / p.prefix_rows);
-        // (chunks of the prefix are at least half a workgroup's share, see Totals: at most 2 * groups tasks more)
+        // (chunks of the prefix have at least a workgroup's share of its units, see Totals: at most `groups` tasks more)
         p.own_parts = (prefix_tasks + 3 * p.groups + 1) * p.prefix_rows;
         p.rows = p.own_parts + ((int64_t)batch * kv_heads * p.own_tiles + p.groups) * p.own_rows;
     }

@@ -90,7 +90,7 @@ constexpr uint32_t group_of(const Deal& d, uint32_t u) {
 // prefix's wait for the matrix units and the others for memory, so a CU has some of
 // both.
 //
-// The prefix is cut into chunks of about a workgroup's share, and its tasks are
+// The prefix is cut into chunks of a workgroup's share of its units, and its tasks are
 // ordered by key/value head, chunk, row tile: workgroups next to each other then run
 // over the same keys at the same time, for other rows, and find them in their XCD's
 // L2.  (With tasks over the whole prefix every workgroup was somewhere else in it:
@@ -113,8 +113,7 @@ constexpr Totals totals(const Split& a, int32_t tokens, uint32_t own_cost) {
         const uint32_t eighths =
             (uint32_t)(((uint64_t)(groups / 8) * cost + (cost + own_cost) / 2) / ((uint64_t)cost + own_cost));
         t.prefix_places = 8 * (eighths < 1 ? 1u : smaller(eighths, groups / 8 - 1));
-        const uint32_t share = cost / smaller(t.prefix_places, cost);
-        t.chunk = share > 2 * kTaskUnits ? share - kTaskUnits : 1 + share / 2;
+        t.chunk = (tasks * units + t.prefix_places - 1) / t.prefix_places;
         t.chunks = (units + t.chunk - 1) / t.chunk;
         t.prefix = deal(tasks * (units + t.chunks * kTaskUnits), t.prefix_places);
     }
