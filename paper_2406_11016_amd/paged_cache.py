@@ -298,7 +298,7 @@ class PagedCache:
         self._tables = Tables(lengths.data_ptr(), counts.data_ptr(), held.data_ptr(), block_table.data_ptr(),
                               free_pages.data_ptr(), free_count.data_ptr(), B, M, N, page_size)
         self._tables_ref = ctypes.byref(self._tables)
-        self._workspaces = {}
+        self._workspaces, self._workspace_of = {}, {}
 
     def _view(self, n: int) -> Tuple[torch.Tensor, torch.Tensor]:
         got = self._views.get(n)
@@ -364,14 +364,22 @@ class PagedCache:
         at = torch.arange(start, end, device=self.device, dtype=torch.int32) % self.page_size
         append(k, v, k_cache, v_cache, (pages * self.page_size + at)[None])
 
+    def _workspace(self, *sizes: int) -> torch.Tensor:
+        """One for each power of two of bytes, and none is given up: captured graphs may hold it."""
+        size = 1 << (attend_workspace_bytes(*sizes) - 1).bit_length()
+        if size not in self._workspaces:
+            self._workspaces[size] = torch.empty(size, dtype=torch.uint8, device=self.device)
+        return self._workspaces[size]
+
     def attend(self, q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, *, scale: Optional[float] = None,
                out: Optional[torch.Tensor] = None) -> torch.Tensor:
-        """Attention of the planned tokens ``q [B, n, q_heads, head_dim]`` (see attend()).  The workspace is kept, one
-        for each head layout, and shared by all layers: calls have to be ordered."""
+        """Attention of the planned tokens ``q [B, n, q_heads, head_dim]`` (see attend()).  The workspaces are kept
+        and shared by all layers: calls have to be ordered."""
+        if q.dim() != 4:
+            raise SpecVerifyError(f"q must be [batch, tokens, q_heads, head_dim]; it is {list(q.shape)}")
         key = (q.shape, k_cache.shape[1])
-        workspace = self._workspaces.get(key)
+        workspace = self._workspace_of.get(key)
         if workspace is None:
-            workspace = self._workspaces[key] = new_attend_workspace(*q.shape[:3], k_cache.shape[1], q.shape[3],
-                                                                     q.device)
+            workspace = self._workspace_of[key] = self._workspace(*q.shape[:3], k_cache.shape[1], q.shape[3])
         return attend(q, k_cache, v_cache, self.block_table, self.lengths, self.counts, prefix_table=self.prefix_table,
                       prefix_len=self.prefix_len, scale=scale, out=out, workspace=workspace)

@@ -179,3 +179,19 @@ def test_refusals_on_the_device():
     cache.plan(n)
     cache.append(k, k, k_cache, v_cache)
     assert not cache.attend(q, k_cache, v_cache).any()
+
+
+def test_workspaces_of_steps_of_many_sizes():
+    """A workspace for each power of two of bytes serves all sizes of a step; the results are attend()'s."""
+    cache = PagedCache(2, num_pages=16, page_size=16, max_pages=6, max_new=80)
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    k, v = (torch.randn(16, K, 16, D, device="cuda", generator=gen).to(DTYPE) for _ in range(2))
+    ended = torch.ones(2, dtype=torch.int32, device="cuda")
+    for n in range(1, 81):
+        cache.plan(n, release=ended)
+        q = torch.randn(2, n, H, D, device="cuda", generator=gen).to(DTYPE)
+        want = paged_cache.attend(q, k, v, cache.block_table, cache.lengths, cache.counts)
+        assert torch.equal(cache.attend(q, k, v), want)
+    assert len(cache._workspaces) <= 8
+    with pytest.raises(binding.SpecVerifyError, match="q must be"):
+        cache.attend(q[0], k, v)
