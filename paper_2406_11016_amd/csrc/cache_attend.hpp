@@ -831,7 +831,7 @@ __global__ void __launch_bounds__(kThreads, (D > 128 ? 1 : 2)) attend_kernel(Att
         if (blockIdx.x < t.own.groups)
             run<T, D, kRows, kJoined>(a, t, t.own, batch, w, smem, wave_stats, &poison_flag, &special_flag);
     } else if (blockIdx.x < t.prefix_places) {
-        const uint32_t w = t.prefix.groups == t.prefix_places ? xcd * (t.prefix_places / 8) + place : blockIdx.x;
+        const uint32_t w = t.prefix.groups + 8 > t.prefix_places ? xcd * (t.prefix_places / 8) + place : blockIdx.x;
         run<T, D, kPrefix, kShared>(a, t, t.prefix, batch, w, smem, wave_stats, &poison_flag, &special_flag);
     } else {
         run<T, D, kRows, kOwn>(a, t, t.own, batch, blockIdx.x - t.prefix_places, smem, wave_stats, &poison_flag,

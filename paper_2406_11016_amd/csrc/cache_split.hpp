@@ -91,9 +91,11 @@ constexpr uint32_t group_of(const Deal& d, uint32_t u) {
 // both.
 //
 // The prefix is cut into chunks of a workgroup's share of its units, and its tasks are
-// ordered by key/value head, chunk, row tile: workgroups next to each other then run
+// ordered by chunk, key/value head, row tile: workgroups next to each other then run
 // over the same keys at the same time, for other rows, and find them in their XCD's
-// L2.  (With tasks over the whole prefix every workgroup was somewhere else in it:
+// L2.  Where chunks that are longer by less than a task's cost make a task a workgroup,
+// they are, and no border cuts a task (the last chunk, the shorter one, comes last).
+// (With tasks over the whole prefix every workgroup was somewhere else in it:
 // 18,432 rows and 16,384 keys read 1.07 GB from behind the L2s, and 0.40 GB so.)
 struct Totals {
     int32_t tokens, prefix_tiles;  // prefix tiles of one key/value head
@@ -112,10 +114,15 @@ constexpr Totals totals(const Split& a, int32_t tokens, uint32_t own_cost) {
         const uint32_t cost = tasks * (units + kTaskUnits);
         const uint32_t eighths =
             (uint32_t)(((uint64_t)(groups / 8) * cost + (cost + own_cost) / 2) / ((uint64_t)cost + own_cost));
-        t.prefix_places = 8 * (eighths < 1 ? 1u : smaller(eighths, groups / 8 - 1));
-        t.chunk = (tasks * units + t.prefix_places - 1) / t.prefix_places;
+        const uint32_t places = 8 * (eighths < 1 ? 1u : smaller(eighths, groups / 8 - 1));
+        const uint32_t fair = (tasks * units + places - 1) / places, most = places / tasks;
+        const uint32_t whole = most == 0 ? units : (units + most - 1) / most;
+        const bool uncut = most != 0 && whole <= fair + kTaskUnits;
+        t.chunk = uncut ? whole : fair;
         t.chunks = (units + t.chunk - 1) / t.chunk;
-        t.prefix = deal(tasks * (units + t.chunks * kTaskUnits), t.prefix_places);
+        const uint32_t used = uncut ? tasks * t.chunks : places;
+        t.prefix_places = (used + 7) / 8 * 8;
+        t.prefix = deal(tasks * (units + t.chunks * kTaskUnits), used);
     }
     t.own = deal(own_cost, groups - t.prefix_places);
     return t;
@@ -151,14 +158,15 @@ struct Segment {
 constexpr Segment prefix_task(const Split& a, const Totals& t, uint32_t u) {
     Segment g{};
     const uint32_t tiles = (uint32_t)t.prefix_tiles, units = (uint32_t)a.prefix_units;
-    const uint32_t head = tiles * (units + t.chunks * kTaskUnits), chunk_cost = (t.chunk + kTaskUnits) * tiles;
-    g.kv_head = (int32_t)(u / head);
-    const uint32_t at = u - (uint32_t)g.kv_head * head, chunk = at / chunk_cost, in_chunk = at - chunk * chunk_cost;
+    const uint32_t tasks = tiles * (uint32_t)a.kv_heads, chunk_cost = (t.chunk + kTaskUnits) * tasks;
+    const uint32_t chunk = u / chunk_cost, in_chunk = u - chunk * chunk_cost;
     g.offset = chunk * t.chunk;
     g.units = smaller(t.chunk, units - g.offset);
-    const uint32_t tile = in_chunk / (g.units + kTaskUnits);
-    g.task = ((uint32_t)g.kv_head * t.chunks + chunk) * tiles + tile;
-    g.task_start = u - (in_chunk - tile * (g.units + kTaskUnits)) + kTaskUnits;
+    const uint32_t task = in_chunk / (g.units + kTaskUnits);
+    g.kv_head = (int32_t)(task / tiles);
+    const uint32_t tile = task - (uint32_t)g.kv_head * tiles;
+    g.task = chunk * tasks + task;
+    g.task_start = u - (in_chunk - task * (g.units + kTaskUnits)) + kTaskUnits;
     g.prefix_units = units;
     g.row0 = (int32_t)tile << a.plan.prefix_shift;
     g.b = -1;
@@ -227,9 +235,9 @@ constexpr int64_t prefix_part(const Split& a, const Totals& t, int32_t kv_head, 
     const uint32_t tiles = (uint32_t)t.prefix_tiles, tile = (uint32_t)r >> a.plan.prefix_shift;
     const uint32_t chunk = k / kChunkParts, offset = chunk * t.chunk;
     const uint32_t units = smaller(t.chunk, (uint32_t)a.prefix_units - offset);
-    const uint32_t start = (uint32_t)kv_head * tiles * ((uint32_t)a.prefix_units + t.chunks * kTaskUnits) +
-                           chunk * (t.chunk + kTaskUnits) * tiles + tile * (units + kTaskUnits) + kTaskUnits;
-    const uint32_t task = ((uint32_t)kv_head * t.chunks + chunk) * tiles + tile;
+    const uint32_t tasks = tiles * (uint32_t)a.kv_heads, in_chunk = (uint32_t)kv_head * tiles + tile;
+    const uint32_t start = chunk * (t.chunk + kTaskUnits) * tasks + in_chunk * (units + kTaskUnits) + kTaskUnits;
+    const uint32_t task = chunk * tasks + in_chunk;
     const uint32_t w = group_of(t.prefix, start) + (k - chunk * kChunkParts);
     if (w > group_of(t.prefix, start + units - 1)) return -1;
     return (int64_t)(task + w) * a.plan.prefix_rows + (r & (a.plan.prefix_rows - 1));

@@ -173,7 +173,7 @@ static void simulate(const Case& c, int id) {
                         uint32_t keys = 0;  // units of the prefix that its parts hold
                         for (uint32_t chunk = 0; chunk < t.chunks; ++chunk) {
                             const uint32_t ptask =
-                                ((uint32_t)kv * t.chunks + chunk) * t.prefix_tiles + flat / plan.prefix_rows;
+                                (chunk * (uint32_t)c.kv_heads + kv) * t.prefix_tiles + flat / plan.prefix_rows;
                             const auto& have = got[std::make_pair(true, ptask)];
                             CHECK(have.size() == 1 || have.size() == 2, "case %d", id);
                             CHECK(tasks.at({true, ptask}).offset == keys, "case %d", id);
