@@ -796,12 +796,18 @@ __device__ __forceinline__ bool segment(Work<D, kKind>& work, char* smem, float 
 template <class T, int D, int WR, Kind kKind>
 __device__ __forceinline__ void run(const AttendArgs& a, const Totals& t, const Deal& deal, const Batch& batch, uint32_t w,
                                     char* smem, float (*wave_stats)[2][32], int* poison_flag, int* special_flag) {
-    if (w >= deal.groups) return;
     Work<D, kKind> work{a, t, batch, (uint32_t)(uintptr_t)(SV_LDS char*)smem, w, group_start(deal, w + 1),
                         {}, 0, false, group_start(deal, w), 0, 0, 0, false};
     bool more = work.advance();
     if (more) work.stage_first();
     while (more) more = segment<T, D, WR>(work, smem, wave_stats, poison_flag, special_flag);
+}
+
+// Workgroups go round the 8 XCDs.  Those of one XCD take adjoining runs of the tasks
+// that share keys, to read them through one L2.
+__device__ __forceinline__ uint32_t place_in_xcd(uint32_t block, uint32_t groups) {
+    const uint32_t xcd = block % 8;
+    return xcd * (groups / 8) + smaller(xcd, groups % 8) + block / 8;
 }
 
 // kPrefix and kRows: waves that split the rows of the prefix's tasks (0: there are
@@ -823,18 +829,15 @@ __global__ void __launch_bounds__(kThreads, (D > 128 ? 1 : 2)) attend_kernel(Att
             a.cum_cost[b] = batch.cum_cost[b];
             if (b == 0) *a.totals = t;
         }
-    // Workgroups go round the 8 XCDs.  Those of one XCD take adjoining runs of the
-    // tasks that share keys, to read them through one L2.
-    const uint32_t xcd = blockIdx.x % 8, place = blockIdx.x / 8;
     if constexpr (kPrefix == 0) {
-        const uint32_t w = t.own.groups % 8 == 0 ? xcd * (t.own.groups / 8) + place : blockIdx.x;
         if (blockIdx.x < t.own.groups)
-            run<T, D, kRows, kJoined>(a, t, t.own, batch, w, smem, wave_stats, &poison_flag, &special_flag);
-    } else if (blockIdx.x < t.prefix_places) {
-        const uint32_t w = t.prefix.groups + 8 > t.prefix_places ? xcd * (t.prefix_places / 8) + place : blockIdx.x;
-        run<T, D, kPrefix, kShared>(a, t, t.prefix, batch, w, smem, wave_stats, &poison_flag, &special_flag);
-    } else {
-        run<T, D, kRows, kOwn>(a, t, t.own, batch, blockIdx.x - t.prefix_places, smem, wave_stats, &poison_flag,
+            run<T, D, kRows, kJoined>(a, t, t.own, batch, place_in_xcd(blockIdx.x, t.own.groups), smem, wave_stats,
+                                      &poison_flag, &special_flag);
+    } else if (blockIdx.x < t.prefix.groups) {
+        run<T, D, kPrefix, kShared>(a, t, t.prefix, batch, place_in_xcd(blockIdx.x, t.prefix.groups), smem, wave_stats,
+                                    &poison_flag, &special_flag);
+    } else if (blockIdx.x - t.prefix.groups < t.own.groups) {
+        run<T, D, kRows, kOwn>(a, t, t.own, batch, blockIdx.x - t.prefix.groups, smem, wave_stats, &poison_flag,
                                &special_flag);
     }
 }

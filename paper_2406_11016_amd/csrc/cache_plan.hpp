@@ -83,22 +83,28 @@ inline int32_t task_rows(int64_t rows, int32_t head_dim) {
     return rows <= 32 ? 32 : rows <= 64 || head_dim > 128 ? 64 : 128;
 }
 
-// Rows of one sequence from which its tasks run over the prefix themselves:
-// their row tiles are nearly full, so that sharing would save nothing and its
-// parts would still be written and read.
-constexpr int64_t kJoinedRows = 512;
+// Whether the sequences' own tasks run over the prefix themselves: their row tiles
+// are of the largest size and nearly full, so that sharing would save no products,
+// and there are enough of them, so that few have to be cut and have parts.  (Time so
+// to time with the prefix's rows pooled, prefixes of 2,000 to 16,384: tiles full, a
+// task for two workgroups, 0.83 to 0.93 at head_dim 128, 0.93 at 256; tiles full, one
+// for four, 1.10 and 1.07; tiles 7/8 full, a task or more a workgroup, 0.74 to 0.91;
+// tiles 3/4 full, 0.79 to 1.08; 9/16 full, 0.94 to 1.44.)
+constexpr bool joined_pays(int64_t tasks, int64_t groups, int64_t rows, int64_t tile_rows) {
+    return 2 * tasks >= groups && 8 * rows >= 7 * ((rows + tile_rows - 1) / tile_rows * tile_rows);
+}
 
 inline AttendPlan attend_plan(int32_t batch, int32_t max_new, int32_t q_heads, int32_t kv_heads, int32_t head_dim,
                               bool prefix) {
     AttendPlan p{};
     const int64_t group = q_heads / kv_heads, rows = max_new * group;
-    p.joined = !prefix || rows >= kJoinedRows;
     p.own_rows = task_rows(rows, head_dim);
     p.own_tiles = (int32_t)((rows + p.own_rows - 1) / p.own_rows);
     p.prefix_rows = task_rows(batch * rows, head_dim);
     p.own_shift = __builtin_ctz((unsigned)p.own_rows);
     p.prefix_shift = __builtin_ctz((unsigned)p.prefix_rows);
     p.groups = head_dim > 128 ? 256 : 512;  // what the 256 CUs hold at a time: one of 128 KiB LDS each, or two of 64
+    p.joined = !prefix || joined_pays((int64_t)batch * kv_heads * p.own_tiles, p.groups, rows, task_rows(1 << 20, head_dim));
     if (p.joined) {
         p.own_parts = 0;
         p.rows = 2 * (int64_t)p.groups * p.own_rows;

@@ -100,8 +100,7 @@ constexpr uint32_t group_of(const Deal& d, uint32_t u) {
 struct Totals {
     int32_t tokens, prefix_tiles;  // prefix tiles of one key/value head
     uint32_t chunk, chunks;        // units of a chunk of the prefix; chunks
-    Deal prefix, own;
-    uint32_t prefix_places;        // workgroups of the grid that are the prefix's, a multiple of 8
+    Deal prefix, own;              // (the grid's first workgroups are the prefix's)
 };
 constexpr Totals totals(const Split& a, int32_t tokens, uint32_t own_cost) {
     Totals t{};
@@ -112,19 +111,18 @@ constexpr Totals totals(const Split& a, int32_t tokens, uint32_t own_cost) {
             (int32_t)(((uint32_t)tokens * (uint32_t)a.group + (uint32_t)a.plan.prefix_rows - 1) >> a.plan.prefix_shift);
         const uint32_t tasks = (uint32_t)t.prefix_tiles * (uint32_t)a.kv_heads, units = (uint32_t)a.prefix_units;
         const uint32_t cost = tasks * (units + kTaskUnits);
-        const uint32_t eighths =
-            (uint32_t)(((uint64_t)(groups / 8) * cost + (cost + own_cost) / 2) / ((uint64_t)cost + own_cost));
+        // (as many in each of the 8 XCDs: 64 sequences of 64 to 144 rows at head_dim 256
+        // behind 16,384 took 117, 140, 180 and 280 us so, 156, 170, 212 and 309 to the nearest number)
+        const uint32_t eighths = (uint32_t)((uint64_t)(groups / 8) * cost / ((uint64_t)cost + own_cost));
         const uint32_t places = 8 * (eighths < 1 ? 1u : smaller(eighths, groups / 8 - 1));
-        const uint32_t fair = (tasks * units + places - 1) / places, most = places / tasks;
+        const uint32_t fair = smaller(units, (tasks * units + places - 1) / places), most = places / tasks;
         const uint32_t whole = most == 0 ? units : (units + most - 1) / most;
         const bool uncut = most != 0 && whole <= fair + kTaskUnits;
         t.chunk = uncut ? whole : fair;
         t.chunks = (units + t.chunk - 1) / t.chunk;
-        const uint32_t used = uncut ? tasks * t.chunks : places;
-        t.prefix_places = (used + 7) / 8 * 8;
-        t.prefix = deal(tasks * (units + t.chunks * kTaskUnits), used);
+        t.prefix = deal(tasks * (units + t.chunks * kTaskUnits), uncut ? tasks * t.chunks : places);
     }
-    t.own = deal(own_cost, groups - t.prefix_places);
+    t.own = deal(own_cost, groups - t.prefix.groups);
     return t;
 }
 

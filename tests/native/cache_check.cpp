@@ -89,8 +89,8 @@ static void simulate(const Case& c, int id) {
     std::map<std::pair<bool, uint32_t>, Segment> tasks;
     std::vector<std::pair<int64_t, int64_t>> places;
     std::map<std::pair<bool, uint32_t>, uint32_t> done;  // units of each task
-    CHECK(t.prefix_places % 8 == 0 && t.prefix.groups <= t.prefix_places, "case %d", id);
-    CHECK(t.prefix_places + t.own.groups <= (uint32_t)plan.groups, "case %d", id);
+    CHECK(t.prefix.groups + t.own.groups <= (uint32_t)plan.groups, "case %d", id);
+    CHECK(t.chunk <= (uint32_t)a.prefix_units || t.prefix.cost == 0, "case %d", id);
     CHECK((t.prefix.cost == 0) == (plan.joined || t.tokens == 0), "case %d", id);
     for (const bool shared : {true, false}) {
     const Deal& d = shared ? t.prefix : t.own;
@@ -236,6 +236,25 @@ static void section_split() {
             if (with_counts && pick(0, 60) == 0) c.counts.back() = c.max_new + 1;                      // bad
         }
         simulate(c, i);
+        ++cases;
+    }
+    // tasks that run over the prefix themselves: many, of nearly full row tiles
+    for (int i = 0; i < 40; ++i) {
+        Case c{};
+        c.head_dim = dims[pick(0, 4)];
+        c.kv_heads = pick(1, 8);
+        c.q_heads = c.kv_heads * pick(1, 4);
+        c.page_size = 64;
+        c.max_new = 128 / (c.q_heads / c.kv_heads) * pick(1, 3);
+        c.batch = 256 / c.kv_heads + pick(1, 9);
+        c.max_pages = 20;
+        c.prefix_len = pick(1, 2000);
+        for (int32_t b = 0; b < c.batch; ++b) {
+            c.lengths.push_back(pick(0, 500));
+            c.counts.push_back(pick(0, 5) == 0 ? pick(-1, 3) : pick(c.max_new - 5, c.max_new));
+        }
+        CHECK(attend_plan(c.batch, c.max_new, c.q_heads, c.kv_heads, c.head_dim, true).joined, "joined case %d", i);
+        simulate(c, 10000 + i);
         ++cases;
     }
     // nothing to do at all

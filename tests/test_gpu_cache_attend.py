@@ -147,6 +147,16 @@ def test_largest_batches(B, D, prefix):
             paged_cache.new_attend_workspace(B + 1, 1, 1, 1, D, "cuda")
 
 
+@pytest.mark.parametrize("B,n,H,K,D,P", [(32, 128, 8, 8, 64, 16), (16, 125, 16, 16, 128, 32), (64, 16, 8, 2, 256, 64),
+                                         (33, 37, 24, 8, 80, 16), (130, 500, 2, 1, 96, 128)])
+@pytest.mark.parametrize("prefix", [1, 64, 333])
+def test_tasks_that_run_over_the_prefix_themselves(B, n, H, K, D, P, prefix):
+    """Many sequences with nearly full row tiles; some have fewer tokens, or none, or nothing cached."""
+    counts = [n if b % 4 else max(0, n - 9 * b) for b in range(B)]
+    x = make(B, n, H, K, D, P, prefix, [(37 * b) % 150 for b in range(B)], counts, "bf16" if B % 2 else "f16", seed=B)
+    check(x, prefix, "bf16" if B % 2 else "f16")
+
+
 def test_nothing_to_do():
     x = make(3, 4, 4, 2, 64, 16, 100, [5, 6, 7], [0, -1, 0], "bf16", seed=1)
     check(x, 100, "bf16")
