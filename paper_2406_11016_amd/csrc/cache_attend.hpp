@@ -2,14 +2,24 @@
 // batch shares, for gfx950 (MI355X): kernels of spec_cache_attend.
 // (Included by the sources of the two storage types.)
 //
-// Work is cut into tasks of up to kRows query rows of one key/value head (a row
+// Work is cut into tasks of up to 128 query rows of one key/value head (a row
 // is a token and one of its heads) against a run of keys, and a task into units
-// of kKeys keys.  The rows of the whole batch share the prefix's tasks; each
-// sequence has tasks of its own for its own keys.  The units of all tasks in
+// of kKeys keys.  The rows of the whole batch share the prefix's tasks, and each
+// sequence has tasks of its own for its own keys (where those are many and full,
+// they take the prefix along, see joined_pays).  The units of all tasks in
 // order are dealt to the grid's workgroups in equal runs, so lengths need not be
 // known on the host and few long sequences fill the chip as well as many short
 // ones; what a workgroup computes of a task is a part (running maximum, sum and
 // unnormalised output of every row), and a second kernel joins a row's parts.
+//
+// What bounds it, at head_dim 128 with 4 heads to a key/value head: many sequences
+// without a prefix, the memory (64 sequences of 0 to 4,096 cached tokens, 815 MB:
+// 165 us, 4.9 TB/s); rows that share many keys, the issue of the matrix
+// and vector instructions by turns (8 sequences of up to 999 tokens behind 2,000, 156
+// GFLOP: 190 us, 820 TFLOP/s; 64 of up to 9 behind 16,384, 124 GFLOP: 147 us, 845); few
+// rows and keys, the latency of a workgroup's run (the batch's sums 2 us, finding the
+// task 1 to 2, its first tiles 3, writing its part 3: one sequence of 11 tokens
+// behind 1,900, 14 us).  The join takes 4 to 17 us.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -120,7 +130,8 @@ __device__ __forceinline__ Sequence sequence(const Batch& batch, int32_t b) {
     return Sequence{uniform(batch.cum_tokens[b + 1]) - uniform(batch.cum_tokens[b]), max(length, 0), length < 0};
 }
 
-// Every workgroup sums the batch for itself (a few loads and one scan).
+// Every workgroup sums the batch for itself (a few loads and one scan: 2 us, less than
+// a launch of its own).
 __device__ __forceinline__ Totals sum_batch(const Split& a, const Batch& batch, uint32_t (*wave_sums)[2]) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int each = (a.batch + kThreads - 1) / kThreads;
@@ -936,6 +947,7 @@ struct Joiner {
 };
 
 // Rows of a batch with a shared prefix: every row has parts of both.  A wave a row.
+// (14,304 rows of about 8 parts, 59 MB: 17 us; 352 rows of 9: 4.3.)
 template <class T, int D>
 __global__ void __launch_bounds__(kThreads) attend_join_rows_kernel(AttendArgs a) {
     const Split& split = a.split;
@@ -962,12 +974,13 @@ __global__ void __launch_bounds__(kThreads) attend_join_rows_kernel(AttendArgs a
 
 // Tasks that the workgroups' borders cut: block x looks at the border before
 // workgroup x + 1, and joins the task that it cuts if it is the first to; block y
-// takes kJoinRows of its rows.  (Of 32,768 rows in two parts each, and of 65,408: 12.9
-// and 31.2 us with 16 rows a block, 13.9 and 34.5 with 8, 16.1 and 32.1 with 32.)
+// takes kJoinRows of its rows.  (Of 32,768 rows in two parts each, and of 65,408: 11.0
+// and 16.4 us with 16 rows a block, 11.5 and 21.7 with 8, 15.6 and 15.9 with 32.)
 constexpr int kJoinRows = 16;
 
 // The same from two parts each, which is what there is where tasks are many: a team of
-// D / 4 lanes a row, and all rows' loads under way at a time.
+// D / 4 lanes a row, and all rows' loads under way at a time.  (Of 32,768 and of 65,408
+// rows: 11.0 and 16.4 us, 4.1 TB/s.)
 template <class T, int D, class RowOut>
 __device__ __forceinline__ void join_two(const AttendArgs& a, int64_t first, int64_t second, int r0, RowOut row_out) {
     constexpr int kLanes = D / 4, kTeams = 64 / kLanes * (kThreads / 64), kEach = (kJoinRows + kTeams - 1) / kTeams;
