@@ -951,7 +951,8 @@ struct Joiner {
 template <class T, int D>
 __global__ void __launch_bounds__(kThreads) attend_join_rows_kernel(AttendArgs a) {
     const Split& split = a.split;
-    const int64_t row = (int64_t)blockIdx.x * (kThreads / 64) + uniform((int32_t)(threadIdx.x >> 6));
+    const int64_t block = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+    const int64_t row = block * (kThreads / 64) + uniform((int32_t)(threadIdx.x >> 6));
     if (row >= (int64_t)split.batch * split.max_new * a.q_heads) return;
     const int head = (int)((uint32_t)row % (uint32_t)a.q_heads);
     const uint32_t flat = (uint32_t)row / (uint32_t)a.q_heads;
@@ -1081,7 +1082,10 @@ sv_status_t launch(const AttendArgs& a, hipStream_t stream) {
     } else {
         constexpr int kRowsBlock = kThreads / 64;
         const int64_t rows = (int64_t)a.split.batch * a.split.max_new * a.q_heads;
-        hipLaunchKernelGGL((attend_join_rows_kernel<T, D>), dim3((uint32_t)((rows + kRowsBlock - 1) / kRowsBlock)),
+        // (one dimension of a launch has fewer than 2^32 threads: 2^26 rows, of the 2^31 that a call may have)
+        const int64_t blocks = (rows + kRowsBlock - 1) / kRowsBlock, most = 1 << 20;
+        hipLaunchKernelGGL((attend_join_rows_kernel<T, D>),
+                           dim3((uint32_t)(blocks < most ? blocks : most), (uint32_t)((blocks + most - 1) / most)),
                            dim3(kThreads), 0, stream, a);
     }
     return hipGetLastError() == hipSuccess ? SV_OK : SV_ERR_HIP;

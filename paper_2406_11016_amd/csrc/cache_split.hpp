@@ -1,6 +1,6 @@
 // How the cache attention's work is cut, in the terms of cache_attend.hpp: rows
 // and row tiles, units of keys, the workgroups' runs of units, and the places of
-// the parts.  Plain constexpr C++17: the kernels call it, and so does a checker
+// the parts.  Plain constexpr C++17: the kernels call it, and so does a test
 // on the CPU (tests/native/cache_check.cpp).
 #pragma once
 

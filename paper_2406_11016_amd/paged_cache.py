@@ -315,7 +315,8 @@ class PagedCache:
         _call(self._index, self._lib.spec_cache_init, "spec_cache_init", self._tables_ref, self.prefix_table.numel())
 
     def set_prefix(self, length: int) -> None:
-        """All sequences begin with the ``length`` tokens in the cache's first pages (token i in slot i)."""
+        """All sequences begin with the ``length`` tokens in the cache's first pages (token i in slot i).  Graphs
+        captured before go on with the length that was set then."""
         if not 0 <= length <= self.prefix_table.numel() * self.page_size:
             raise SpecVerifyError(f"a prefix of {length} tokens does not fit {self.prefix_table.numel()} pages")
         self.prefix_len = length

@@ -157,6 +157,35 @@ def test_tasks_that_run_over_the_prefix_themselves(B, n, H, K, D, P, prefix):
     check(x, prefix, "bf16" if B % 2 else "f16")
 
 
+def test_more_rows_than_a_launch_has_waves_in_one_dimension():
+    """4096 x 513 x 32 rows of q, of which four sequences have a few tokens."""
+    if torch.cuda.mem_get_info()[0] < 80 << 30:
+        pytest.skip("needs 60 GB of memory")
+    B, n, H, D = 4096, 513, 32, 64
+    some = [0, 1, 2049, B - 1]
+    x = make(len(some), n, H, H, D, 16, 20, [5, 0, 30, 17], [3, 1, 2, 5], "bf16", seed=11)
+    q, k, v, table, lengths, counts, prefix_table = x
+    at = torch.tensor(some, device="cuda")
+
+    def spread(small, fill):
+        big = torch.full((B, *small.shape[1:]), fill, dtype=small.dtype, device="cuda")
+        big[at] = small
+        return big
+
+    out = torch.full((B, n, H, D), KEPT, dtype=q.dtype, device="cuda")
+    paged_cache.attend(spread(q, float("nan")), k, v, spread(table, -1), spread(lengths, 3), spread(counts, 0),
+                       prefix_table=prefix_table, prefix_len=20, out=out)
+    want, size, product = attend_reference(q, k, v, table.cpu().numpy(), lengths.tolist(), counts.tolist(),
+                                           prefix_table.cpu().numpy(), 20, D ** -0.5)
+    bound = attend_bound(size, product, "bf16", D, 60, float(torch.nan_to_num(v.float(), 0.0).abs().max()))
+    got = out[at].double().cpu().numpy()
+    for i, m in enumerate(counts.tolist()):
+        assert np.all(np.abs(got[i, :m] - want[i, :m]) <= bound[i, :m]), some[i]
+    for b in range(B):
+        first = counts[some.index(b)].item() if b in some else 0
+        assert bool((out[b, first:] == KEPT).all()), b
+
+
 def test_nothing_to_do():
     x = make(3, 4, 4, 2, 64, 16, 100, [5, 6, 7], [0, -1, 0], "bf16", seed=1)
     check(x, 100, "bf16")
