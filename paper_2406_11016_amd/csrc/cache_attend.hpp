@@ -902,11 +902,14 @@ struct Joiner {
         part_sum = lane < count ? a.part_sum[at] : 0.0f;
         load(0);
     }
-    // Joins what was fetched, and the parts behind it, and writes the row.
-    template <class T, class Place>
-    __device__ __forceinline__ void join(int n, Place place, uint16_t* to) {
-        float top = -INFINITY, sum = 0.0f;
-        f32x4 out = f32x4(0.0f);
+    // Joins what was fetched, and the parts behind it: maximum, sum and, in the first kLanes lanes, output.
+    float top, sum;
+    f32x4 out;
+    template <class Place>
+    __device__ __forceinline__ void join(int n, Place place) {
+        top = -INFINITY;
+        sum = 0.0f;
+        out = f32x4(0.0f);
         for (int base = 0;;) {
             if (count > 0) {
                 float now = fmaxf(top, most);
@@ -940,19 +943,65 @@ struct Joiner {
         for (int t = 1; t < kTeams; ++t)
 #pragma unroll
             for (int e = 0; e < 4; ++e) all[e] += __shfl(out[e], (lane + t * kLanes) & 63);
+        out = all;
+    }
+    template <class T>
+    __device__ __forceinline__ void write(uint16_t* to) const {
         if (lane >= kLanes) return;
-        all *= 1.0f / sum;
-        *(u32x2*)(to + d) = __builtin_bit_cast(u32x2, __builtin_convertvector(all, typename T::V4));
+        *(u32x2*)(to + d) = __builtin_bit_cast(u32x2, __builtin_convertvector(out * (1.0f / sum), typename T::V4));
     }
 };
 
+// One row from many parts, by a workgroup: its waves join every fourth part, and the
+// first wave joins those.
+template <class T, int D, class Place>
+__device__ __forceinline__ void join_by_block(const AttendArgs& a, int n, Place place, uint16_t* to, float (*box)[D + 4]) {
+    constexpr int kWaves = kThreads / 64;
+    const int wave = uniform((int32_t)(threadIdx.x >> 6));
+    auto every = [&](int k) { return place(kWaves * k + wave); };
+    const int parts = (n - wave + kWaves - 1) / kWaves;
+    Joiner<D> own(a);
+    own.fetch(0, parts, every);
+    own.join(parts, every);
+    if (own.lane < Joiner<D>::kLanes) *(f32x4*)&box[wave][own.d] = own.out;
+    if (own.lane == 0) {
+        box[wave][D] = own.top;
+        box[wave][D + 1] = own.sum;
+    }
+    __syncthreads();
+    if (wave == 0) {
+        float now = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) now = fmaxf(now, box[w][D]);
+        const float ref = now == -INFINITY ? 0.0f : now;
+        own.sum = 0.0f;
+        own.out = f32x4(0.0f);
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            const float by = exp2_hw(box[w][D] - ref);
+            own.sum += by * box[w][D + 1];
+            own.out += by * *(const f32x4*)&box[w][own.d];
+        }
+        own.template write<T>(to);
+    }
+    __syncthreads();  // the box is free again
+}
+
+// Parts from which a row is joined by a workgroup, not by a wave, and behind a prefix
+// rows up to which it is.  (One sequence of 30,000 keys, 8 to 64 rows at head_dim 256, 256
+// parts: 27 to 42 us with the attention, and 55 to 78 by waves; behind 4,000 keys 20 to 23,
+// and 25 to 29.  But 2,048 rows of about 32 parts: 43, and 40 by waves.)
+constexpr int kBlockParts = 16;
+constexpr int64_t kBlockRows = 1024;
+
 // Rows of a batch with a shared prefix: every row has parts of both.  A wave a row.
 // (14,304 rows of about 8 parts, 59 MB: 17 us; 352 rows of 9: 4.3.)
-template <class T, int D>
+template <class T, int D, bool kBlock>
 __global__ void __launch_bounds__(kThreads) attend_join_rows_kernel(AttendArgs a) {
+    __shared__ __attribute__((aligned(16))) float box[kBlock ? kThreads / 64 : 1][D + 4];
     const Split& split = a.split;
     const int64_t block = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
-    const int64_t row = block * (kThreads / 64) + uniform((int32_t)(threadIdx.x >> 6));
+    const int64_t row = kBlock ? block : block * (kThreads / 64) + uniform((int32_t)(threadIdx.x >> 6));
     if (row >= (int64_t)split.batch * split.max_new * a.q_heads) return;
     const int head = (int)((uint32_t)row % (uint32_t)a.q_heads);
     const uint32_t flat = (uint32_t)row / (uint32_t)a.q_heads;
@@ -967,15 +1016,20 @@ __global__ void __launch_bounds__(kThreads) attend_join_rows_kernel(AttendArgs a
     auto place = [&](int k) {
         return k < prefix ? prefix_part(split, t, kv_head, r, (uint32_t)k) : own.first + (k - prefix) * own.step;
     };
-    Joiner<D> parts(a);
-    parts.fetch(0, prefix + own.n, place);
-    parts.template join<T>(prefix + own.n, place,
-                           a.out + b * a.out_stride[0] + token * a.out_stride[1] + head * a.out_stride[2]);
+    uint16_t* const to = a.out + b * a.out_stride[0] + token * a.out_stride[1] + head * a.out_stride[2];
+    if constexpr (kBlock) {
+        join_by_block<T, D>(a, prefix + own.n, place, to, box);
+    } else {
+        Joiner<D> parts(a);
+        parts.fetch(0, prefix + own.n, place);
+        parts.join(prefix + own.n, place);
+        parts.template write<T>(to);
+    }
 }
 
 // Tasks that the workgroups' borders cut: block x looks at the border before
-// workgroup x + 1, and joins the task that it cuts if it is the first to; block y
-// takes kJoinRows of its rows.  (Of 32,768 rows in two parts each, and of 65,408: 11.0
+// workgroup x + 1; the blocks of the borders that cut a task share its rows, of which
+// block y has kJoinRows.  (Of 32,768 rows in two parts each, and of 65,408: 11.0
 // and 16.4 us with 16 rows a block, 11.5 and 21.7 with 8, 15.6 and 15.9 with 32.)
 constexpr int kJoinRows = 16;
 
@@ -1017,15 +1071,17 @@ __device__ __forceinline__ void join_two(const AttendArgs& a, int64_t first, int
 }
 template <class T, int D>
 __global__ void __launch_bounds__(kThreads) attend_join_tasks_kernel(AttendArgs a) {
+    __shared__ __attribute__((aligned(16))) float box[kThreads / 64][D + 4];
     const Split& split = a.split;
     const Totals& t = *a.totals;
     const uint32_t w = blockIdx.x + 1;
     if (w >= t.own.groups) return;
     const Segment g = own_task_at(split, a.cum_cost, group_start(t.own, w), [&](int32_t b) { return sequence(split, b); });
     uint32_t w0, w1;
-    if (!first_border(t, g, w, w0, w1)) return;
-    const int n = 1 + (int)(w1 - w0), end = (int)(blockIdx.y + 1) * kJoinRows;
-    int r = (int)blockIdx.y * kJoinRows + uniform((int32_t)(threadIdx.x >> 6));
+    if (!cuts_task(t, g, w, w0, w1)) return;
+    const int borders = (int)(w1 - w0), n = 1 + borders, mine = (int)(w - w0) - 1;
+    const int end = (int)(blockIdx.y + 1) * kJoinRows;
+    int r = (int)blockIdx.y * kJoinRows;  // (`place` is that of row r)
     auto row_out = [&](int of) -> uint16_t* {
         const int row = g.row0 + of, token = row / split.group;
         const int head = g.kv_head * split.group + (row - token * split.group);
@@ -1040,13 +1096,23 @@ __global__ void __launch_bounds__(kThreads) attend_join_tasks_kernel(AttendArgs 
         const Parts first = first_cut_part(split, w0, r), later = later_cut_parts(split, w0, w1, r);
         return k == 0 ? first.first : later.first + (k - 1) * later.step;
     };
+    if (n >= kBlockParts) {
 #pragma unroll 1
-    for (; r < end; r += kThreads / 64) {
+        for (r += mine; r < end; r += borders) {
+            uint16_t* const to = row_out(r);
+            if (to == nullptr) return;
+            join_by_block<T, D>(a, n, place, to, box);
+        }
+        return;
+    }
+#pragma unroll 1
+    for (r += mine * (kThreads / 64) + uniform((int32_t)(threadIdx.x >> 6)); r < end; r += borders * (kThreads / 64)) {
         uint16_t* const to = row_out(r);
         if (to == nullptr) return;
         Joiner<D> parts(a);
         parts.fetch(0, n, place);
-        parts.template join<T>(n, place, to);
+        parts.join(n, place);
+        parts.template write<T>(to);
     }
 }
 
@@ -1082,11 +1148,14 @@ sv_status_t launch(const AttendArgs& a, hipStream_t stream) {
     } else {
         constexpr int kRowsBlock = kThreads / 64;
         const int64_t rows = (int64_t)a.split.batch * a.split.max_new * a.q_heads;
+        const bool by_block = rows <= kBlockRows && (int64_t)groups >= kBlockParts * pooled_tasks(a.split);
         // (one dimension of a launch has fewer than 2^32 threads: 2^26 rows, of the 2^31 that a call may have)
-        const int64_t blocks = (rows + kRowsBlock - 1) / kRowsBlock, most = 1 << 20;
-        hipLaunchKernelGGL((attend_join_rows_kernel<T, D>),
-                           dim3((uint32_t)(blocks < most ? blocks : most), (uint32_t)((blocks + most - 1) / most)),
-                           dim3(kThreads), 0, stream, a);
+        const int64_t blocks = by_block ? rows : (rows + kRowsBlock - 1) / kRowsBlock, most = 1 << 20;
+        const dim3 grid((uint32_t)(blocks < most ? blocks : most), (uint32_t)((blocks + most - 1) / most));
+        if (by_block)
+            hipLaunchKernelGGL((attend_join_rows_kernel<T, D, true>), grid, dim3(kThreads), 0, stream, a);
+        else
+            hipLaunchKernelGGL((attend_join_rows_kernel<T, D, false>), grid, dim3(kThreads), 0, stream, a);
     }
     return hipGetLastError() == hipSuccess ? SV_OK : SV_ERR_HIP;
 }

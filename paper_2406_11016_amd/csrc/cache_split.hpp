@@ -126,6 +126,11 @@ constexpr Totals totals(const Split& a, int32_t tokens, uint32_t own_cost) {
     return t;
 }
 
+// Tasks of the prefix, uncut, if every sequence has max_new tokens.
+constexpr int64_t pooled_tasks(const Split& a) {
+    return (int64_t)a.kv_heads * (((int64_t)a.batch * a.max_new * a.group + a.plan.prefix_rows - 1) >> a.plan.prefix_shift);
+}
+
 // The last b of n with cum[b] <= x (cum[0] <= x < cum[n]).
 template <class I>
 constexpr int32_t find(const I* cum, int32_t n, I x) {
@@ -258,12 +263,12 @@ constexpr Parts own_parts(const Split& a, const Totals& t, const Sequence& s, ui
                  a.plan.own_rows, (int32_t)(w1 - w0) + 1};
 }
 
-// Without one: whether the border before workgroup w (w > 0) is the first to cut a
-// task's units, and then the workgroups that have parts of it.
-constexpr bool first_border(const Totals& t, const Segment& g, uint32_t w, uint32_t& w0, uint32_t& w1) {
+// Without one: whether the border before workgroup w (w > 0) cuts a task's units, and
+// then the first and last of the workgroups that have parts of it (w0 < w <= w1).
+constexpr bool cuts_task(const Totals& t, const Segment& g, uint32_t w, uint32_t& w0, uint32_t& w1) {
     w0 = group_of(t.own, g.task_start);
     w1 = group_of(t.own, g.task_start + g.units - 1);
-    return group_start(t.own, w) > g.task_start && w == w0 + 1;
+    return group_start(t.own, w) > g.task_start;
 }
 // Row r of a task cut by the borders of workgroups w0 .. w1; the
 // first one's part is its last segment's, the others' are their first ones'.

@@ -193,17 +193,23 @@ static void simulate(const Case& c, int id) {
                     } else if (got.count({false, task})) {
                         const auto& have = got[std::make_pair(false, task)];
                         uint32_t w0 = 0, w1 = 0;
-                        CHECK(first_border(t, g, group_of(t.own, g.task_start) + 1, w0, w1), "case %d", id);
+                        CHECK(cuts_task(t, g, group_of(t.own, g.task_start) + 1, w0, w1), "case %d", id);
                         CHECK(w1 > w0 && have.size() == w1 - w0 + 1, "case %d", id);
                         same(first_cut_part(a, w0, r % plan.own_rows), have, 0, r % plan.own_rows);
                         same(later_cut_parts(a, w0, w1, r % plan.own_rows), have, 1, r % plan.own_rows);
-                        // one workgroup of the joining kernel takes it
+                        // the workgroups of the joining kernel that take it, and no other
+                        uint32_t borders = 0;
                         for (uint32_t w = 1; w < t.own.groups && r % plan.own_rows == 0; ++w) {
                             const uint32_t u = group_start(t.own, w);
                             if (u + kTaskUnits < g.task_start || u >= g.task_start + g.units) continue;
                             uint32_t x0, x1;
-                            CHECK(first_border(t, g, w, x0, x1) == (w == w0 + 1), "case %d", id);
+                            CHECK(cuts_task(t, g, w, x0, x1) == (w > w0 && w <= w1), "case %d", id);
+                            if (cuts_task(t, g, w, x0, x1)) {
+                                CHECK(x0 == w0 && x1 == w1, "case %d", id);
+                                ++borders;
+                            }
                         }
+                        CHECK(r % plan.own_rows != 0 || borders == w1 - w0, "case %d", id);
                     } else {
                         CHECK(group_of(t.own, g.task_start) == group_of(t.own, g.task_start + g.units - 1), "case %d", id);
                     }

@@ -157,6 +157,16 @@ def test_tasks_that_run_over_the_prefix_themselves(B, n, H, K, D, P, prefix):
     check(x, prefix, "bf16" if B % 2 else "f16")
 
 
+@pytest.mark.parametrize("n", [1, 5, 30])
+@pytest.mark.parametrize("H,K,D", [(8, 1, 256), (4, 2, 128), (2, 1, 80)])
+def test_rows_of_many_parts(H, K, D, n):
+    """One long sequence, or a few behind a long prefix: a row's keys are shared out to most workgroups."""
+    x = make(1, n, H, K, D, 64, 0, [20011], [n], "bf16", seed=n)
+    check(x, 0, "bf16")
+    x = make(3, n, H, K, D, 64, 15005, [300, 0, 9000], [n, 0, max(1, n - 2)], "f16", seed=n)
+    check(x, 15005, "f16")
+
+
 def test_more_rows_than_a_launch_has_waves_in_one_dimension():
     """4096 x 513 x 32 rows of q, of which four sequences have a few tokens."""
     if torch.cuda.mem_get_info()[0] < 80 << 30:
