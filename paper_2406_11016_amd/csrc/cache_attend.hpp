@@ -19,7 +19,7 @@
 // GFLOP: 190 us, 820 TFLOP/s; 64 of up to 9 behind 16,384, 124 GFLOP: 147 us, 845); few
 // rows and keys, the latency of a workgroup's run (the batch's sums 2 us, finding the
 // task 1 to 2, its first tiles 3, writing its part 3: one sequence of 11 tokens
-// behind 1,900, 14 us).  The join takes 4 to 17 us.
+// behind 1,900, 14 us).  The join takes 3 to 18 us.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -1035,7 +1035,7 @@ constexpr int kJoinRows = 16;
 
 // The same from two parts each, which is what there is where tasks are many: a team of
 // D / 4 lanes a row, and all rows' loads under way at a time.  (Of 32,768 and of 65,408
-// rows: 11.0 and 16.4 us, 4.1 TB/s.)
+// rows: 9.1 and 16.3 us, 4.1 TB/s.)
 template <class T, int D, class RowOut>
 __device__ __forceinline__ void join_two(const AttendArgs& a, int64_t first, int64_t second, int r0, RowOut row_out) {
     constexpr int kLanes = D / 4, kTeams = 64 / kLanes * (kThreads / 64), kEach = (kJoinRows + kTeams - 1) / kTeams;
