@@ -36,6 +36,9 @@ sequence, keeping what the last iteration accepted -- one launch on the loop's
 stream, from the accepted lengths where they are.  The producer writes and reads
 the cache through ``loop.cache`` (``append``, ``attend``, ``positions``).  The
 first iteration keeps everything that the program planned before (its prompts).
+Where an iteration ends with an exception -- the producer's, or a step's whose
+results are not valid -- nothing that was planned for it stays in the cache, and
+``loop.acc`` is -1 throughout.
 """
 from __future__ import annotations
 
@@ -107,6 +110,7 @@ class DecodeLoop:
                              f"it has {cache.batch}, {cache.max_new} on {cache.device}")
         self.cache = cache
         self._keep_all = True   # the next iteration keeps all that was planned last (not: what it accepted)
+        self._unverified = False   # the loop's last plan has had no step yet
         tdt = STORAGE_TORCH_DTYPES[dtype]
         B, G, V = batch, gamma_max, vocab
         self.draft = torch.empty(B * G * V, dtype=tdt, device=self.device)
@@ -192,6 +196,7 @@ class DecodeLoop:
         else:
             with torch.cuda.stream(self.stream):
                 self._call(gamma, early)
+        self._unverified = False
 
     def collect(self) -> Tuple[np.ndarray, np.ndarray]:
         """Wait for the launched call; its accepted lengths and next tokens."""
@@ -203,6 +208,8 @@ class DecodeLoop:
                                  non_blocking=True)
         self.stream.synchronize()
         if int(self.flag_host[0]) != 0:
+            if self.cache is not None:
+                self.discard_step()
             raise binding.SpecVerifyError("a wait between workgroups timed out: the outputs are not valid; "
                                           "re-initialise the workspace (reset_workspace)")
         h = self.host.numpy()
@@ -216,15 +223,27 @@ class DecodeLoop:
 
     # -- the target model's cache ----------------------------------------------
     def plan_cache(self, gamma: int) -> None:
-        """Enqueue the plan of an iteration's gamma + 1 tokens a sequence (run() does it before each producer)."""
+        """Enqueue the plan of an iteration's gamma + 1 tokens a sequence (run() does it before each producer).  It
+        keeps what the step of the last plan accepted; nothing, if there was no such step."""
+        if self._unverified:
+            self.discard_step()
         with torch.cuda.stream(self.stream):
             self.cache.plan(gamma + 1, accepted_len=None if self._keep_all else self.acc)
         self._keep_all = False
+        self._unverified = True
+
+    def discard_step(self) -> None:
+        """The step that was planned last has no valid results: the next plan, the loop's or the program's with
+        ``accepted_len=loop.acc``, keeps none of its tokens (run() does it where an iteration raises)."""
+        with torch.cuda.stream(self.stream):
+            self.acc.fill_(-1)
+        self._unverified = False
 
     def program_planned(self) -> None:
         """Between runs, after the program has planned for itself with ``accepted_len=loop.acc`` (new sequences'
         prompts, say): the next iteration keeps all the tokens of that plan."""
         self._keep_all = True
+        self._unverified = False
 
     def run(self, producer, iterations: int, stats: Optional[LoopStats] = None,
             time_device: bool = False) -> LoopStats:
@@ -235,41 +254,50 @@ class DecodeLoop:
         gamma = self.gamma0
         ev = (torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)) if time_device else None
         for i in range(iterations):
-            if self.cache is not None:
-                self.plan_cache(gamma)
-            producer(self, i, gamma)
-            if self.native is not None:
-                nxt_gamma = binding.loop_step(self.native, gamma)
-                h = self.host.numpy()
-                L, nx = h[:self.B].copy(), h[self.B:].copy()
-                stats.early_exit.append(binding.loop_last_early_exit(self.native) == 1)
-                stats.iterations += 1
-                stats.gammas.append(gamma)
-                stats.accepted.append(L)
-                stats.next_tokens.append(nx)
-                stats.tokens += int(np.sum(np.where(L >= 0, L + 1, 0)))
-                gamma = nxt_gamma
+            if self.cache is None:
+                gamma = self._iterate(producer, i, gamma, stats, ev)
                 continue
-            early = self._early_next
-            if ev is not None:
-                ev[0].record(self.stream)
-            self.launch(gamma, early)
-            if ev is not None:
-                ev[1].record(self.stream)
-            L, nx = self.collect()
-            stats.early_exit.append(early)
-            if self.mode == "exact" and self.early_exit == "auto":
-                self._early_next = early_exit_pays(L, gamma)
-            if ev is not None:
-                stats.device_us.append(ev[0].elapsed_time(ev[1]) * 1000.0)
+            self.plan_cache(gamma)
+            try:
+                gamma = self._iterate(producer, i, gamma, stats, ev)
+            except BaseException:
+                self.discard_step()
+                raise
+        return stats
+
+    def _iterate(self, producer, i: int, gamma: int, stats: LoopStats, ev) -> int:
+        """One producer and step; the next gamma."""
+        producer(self, i, gamma)
+        if self.native is not None:
+            nxt_gamma = binding.loop_step(self.native, gamma)
+            self._unverified = False
+            h = self.host.numpy()
+            L, nx = h[:self.B].copy(), h[self.B:].copy()
+            stats.early_exit.append(binding.loop_last_early_exit(self.native) == 1)
             stats.iterations += 1
             stats.gammas.append(gamma)
             stats.accepted.append(L)
             stats.next_tokens.append(nx)
             stats.tokens += int(np.sum(np.where(L >= 0, L + 1, 0)))
-            if self.adapt_gamma:
-                gamma = next_gamma(gamma, L, self.gamma_max)
-        return stats
+            return nxt_gamma
+        early = self._early_next
+        if ev is not None:
+            ev[0].record(self.stream)
+        self.launch(gamma, early)
+        if ev is not None:
+            ev[1].record(self.stream)
+        L, nx = self.collect()
+        stats.early_exit.append(early)
+        if self.mode == "exact" and self.early_exit == "auto":
+            self._early_next = early_exit_pays(L, gamma)
+        if ev is not None:
+            stats.device_us.append(ev[0].elapsed_time(ev[1]) * 1000.0)
+        stats.iterations += 1
+        stats.gammas.append(gamma)
+        stats.accepted.append(L)
+        stats.next_tokens.append(nx)
+        stats.tokens += int(np.sum(np.where(L >= 0, L + 1, 0)))
+        return next_gamma(gamma, L, self.gamma_max) if self.adapt_gamma else gamma
 
 
 class SyntheticSteps:
