@@ -159,17 +159,19 @@ class DecodeLoop:
         return (self.draft[:B * gamma * V].view(B, gamma, V), self.target[:B * (gamma + 1) * V].view(B, gamma + 1, V),
                 self.tokens[:B * gamma].view(B, gamma), self.uniforms[:B * (gamma + 1)].view(B, gamma + 1))
 
-    def _call(self, gamma: int, early: bool = False) -> None:
+    def _call(self, gamma: int, early: bool = False, acc: Optional[torch.Tensor] = None,
+              nxt: Optional[torch.Tensor] = None) -> None:
         d, t, tok, u = self.views(gamma)
         binding.verify(d, t, tok, u, mode=self.mode, temperature=self.temperature, alpha=self.alpha,
-                       beta=self.beta, accepted_len=self.acc, next_token=self.nxt, workspace=self.ws,
-                       early_exit=early)
+                       beta=self.beta, accepted_len=self.acc if acc is None else acc,
+                       next_token=self.nxt if nxt is None else nxt, workspace=self.ws, early_exit=early)
 
     def _graph(self, gamma: int, early: bool = False) -> torch.cuda.CUDAGraph:
         g = self.graphs.get((gamma, early))
         if g is None:
             with torch.cuda.stream(self.stream):
-                self._call(gamma, early)   # eager once on the capture stream (checks the arguments)
+                # eager once on the capture stream (checks the arguments), the last step's results left as they are
+                self._call(gamma, early, torch.empty_like(self.acc), torch.empty_like(self.nxt))
             self.stream.synchronize()
             g = torch.cuda.CUDAGraph()
             with torch.cuda.graph(g, stream=self.stream):

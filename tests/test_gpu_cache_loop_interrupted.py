@@ -135,3 +135,22 @@ def test_steps_driven_by_hand():
             loop.collect()
     _lengths_agree(model)
     loop.close()
+
+
+@pytest.mark.parametrize("graphs", [False, True])
+def test_capturing_between_runs_leaves_the_accepted_lengths(graphs):
+    """capture_all() checks each call's arguments by running it; the last step's results stay what they are."""
+    model = _model(False, graphs)
+    loop = model.loop
+    stats = loop.run(model, 3)
+    loop.uniforms.fill_(1.0)       # (a step on the buffers as they are now would accept other lengths)
+    loop.tokens.fill_(3)
+    torch.cuda.synchronize()
+    loop.capture_all()
+    torch.cuda.synchronize()
+    assert loop.acc.tolist() == stats.accepted[-1].tolist() and loop.nxt.tolist() == stats.next_tokens[-1].tolist()
+    _settle(model)
+    model.pending = None
+    loop.run(model, 2)
+    _lengths_agree(model)
+    loop.close()
