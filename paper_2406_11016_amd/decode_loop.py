@@ -38,7 +38,10 @@ the cache through ``loop.cache`` (``append``, ``attend``, ``positions``).  The
 first iteration keeps everything that the program planned before (its prompts).
 Where an iteration ends with an exception -- the producer's, or a step's whose
 results are not valid -- nothing that was planned for it stays in the cache, and
-``loop.acc`` is -1 throughout.
+``loop.acc`` is -1 throughout.  A sequence that a plan could not serve (no free
+pages, or its table is full) takes no part in that iteration: its accepted
+length and next token are -1, in the results and in ``loop.acc``, it counts as
+not accepted, and its cache stays as it is until a plan serves it again.
 """
 from __future__ import annotations
 
@@ -81,6 +84,7 @@ class LoopStats:
     next_tokens: List[np.ndarray] = field(default_factory=list)
     device_us: List[float] = field(default_factory=list)   # per iteration, when timed
     early_exit: List[bool] = field(default_factory=list)   # per iteration: the early exit ran
+    unserved: List[np.ndarray] = field(default_factory=list)  # with a cache, per iteration: [B], True: not served
 
 
 class DecodeLoop:
@@ -111,6 +115,8 @@ class DecodeLoop:
         self.cache = cache
         self._keep_all = True   # the next iteration keeps all that was planned last (not: what it accepted)
         self._unverified = False   # the loop's last plan has had no step yet
+        # what the loop's last plan gave, in pinned memory: there by the time that its step's results are
+        self._counts_host = None if cache is None else torch.zeros(batch, dtype=torch.int32, pin_memory=True)
         tdt = STORAGE_TORCH_DTYPES[dtype]
         B, G, V = batch, gamma_max, vocab
         self.draft = torch.empty(B * G * V, dtype=tdt, device=self.device)
@@ -215,7 +221,9 @@ class DecodeLoop:
             raise binding.SpecVerifyError("a wait between workgroups timed out: the outputs are not valid; "
                                           "re-initialise the workspace (reset_workspace)")
         h = self.host.numpy()
-        return h[:B].copy(), h[B:].copy()
+        L, nx = h[:B].copy(), h[B:].copy()
+        self._drop_unserved(L, nx)
+        return L, nx
 
     def reset_workspace(self) -> None:
         """Zero-fill the workspace (after a timed-out wait)."""
@@ -225,14 +233,27 @@ class DecodeLoop:
 
     # -- the target model's cache ----------------------------------------------
     def plan_cache(self, gamma: int) -> None:
-        """Enqueue the plan of an iteration's gamma + 1 tokens a sequence (run() does it before each producer).  It
-        keeps what the step of the last plan accepted; nothing, if there was no such step."""
+        """Enqueue the plan of an iteration's gamma + 1 tokens a sequence (run() does it before each producer; by hand,
+        after the last step's collect()).  It keeps what the step of the last plan accepted; nothing, if there was no
+        such step."""
         if self._unverified:
             self.discard_step()
         with torch.cuda.stream(self.stream):
             self.cache.plan(gamma + 1, accepted_len=None if self._keep_all else self.acc)
+            self._counts_host.copy_(self.cache.counts, non_blocking=True)
         self._keep_all = False
         self._unverified = True
+
+    def _drop_unserved(self, L: np.ndarray, nx: np.ndarray) -> Optional[np.ndarray]:
+        """After a step's wait: no results for the sequences that the last plan could not serve, and which those are."""
+        if self.cache is None:
+            return None
+        unserved = self._counts_host.numpy() < 0
+        if unserved.any():
+            L[unserved] = nx[unserved] = -1
+            with torch.cuda.stream(self.stream):
+                self.acc.masked_fill_(self.cache.counts < 0, -1)
+        return unserved
 
     def discard_step(self) -> None:
         """The step that was planned last has no valid results: the next plan, the loop's or the program's with
@@ -275,6 +296,11 @@ class DecodeLoop:
             self._unverified = False
             h = self.host.numpy()
             L, nx = h[:self.B].copy(), h[self.B:].copy()
+            unserved = self._drop_unserved(L, nx)
+            if unserved is not None:
+                stats.unserved.append(unserved)
+                if unserved.any():   # (the library's rule took their lengths for results)
+                    nxt_gamma = next_gamma(gamma, L, self.gamma_max)
             stats.early_exit.append(binding.loop_last_early_exit(self.native) == 1)
             stats.iterations += 1
             stats.gammas.append(gamma)
@@ -289,6 +315,8 @@ class DecodeLoop:
         if ev is not None:
             ev[1].record(self.stream)
         L, nx = self.collect()
+        if self.cache is not None:
+            stats.unserved.append(self._counts_host.numpy() < 0)
         stats.early_exit.append(early)
         if self.mode == "exact" and self.early_exit == "auto":
             self._early_next = early_exit_pays(L, gamma)
