@@ -42,6 +42,10 @@ results are not valid -- nothing that was planned for it stays in the cache, and
 pages, or its table is full) takes no part in that iteration: its accepted
 length and next token are -1, in the results and in ``loop.acc``, it counts as
 not accepted, and its cache stays as it is until a plan serves it again.
+
+The loop works on a stream of its own, ``loop.stream``.  run() begins behind what
+the current stream holds when it is called (the program's plans, its cache), and
+what the program enqueues there afterwards runs behind the loop's work.
 """
 from __future__ import annotations
 
@@ -130,6 +134,7 @@ class DecodeLoop:
         ws = max(binding.workspace_bytes(B, g, V, tdt) for g in range(1, G + 1))
         self.ws = torch.zeros((ws + 15) // 16 * 16, dtype=torch.uint8, device=self.device)
         self.stream = torch.cuda.Stream(self.device)
+        self._follow()   # (the buffers are filled on the current stream)
         self.graphs: Dict[Tuple[int, bool], torch.cuda.CUDAGraph] = {}
         # the native loop: one library call per iteration (graph replay or
         # launch, the transfer of the results, the wait and the gamma rule)
@@ -154,6 +159,10 @@ class DecodeLoop:
             self.close()
         except Exception:
             pass
+
+    def _follow(self) -> None:
+        """The loop's stream goes on behind the current one."""
+        self.stream.wait_stream(torch.cuda.current_stream(self.stream.device))
 
     # -- the buffers an iteration's producer writes ---------------------------
     def views(self, gamma: int) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor, torch.Tensor]:
@@ -276,16 +285,20 @@ class DecodeLoop:
         stats = stats or LoopStats()
         gamma = self.gamma0
         ev = (torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)) if time_device else None
-        for i in range(iterations):
-            if self.cache is None:
-                gamma = self._iterate(producer, i, gamma, stats, ev)
-                continue
-            self.plan_cache(gamma)
-            try:
-                gamma = self._iterate(producer, i, gamma, stats, ev)
-            except BaseException:
-                self.discard_step()
-                raise
+        self._follow()
+        try:
+            for i in range(iterations):
+                if self.cache is None:
+                    gamma = self._iterate(producer, i, gamma, stats, ev)
+                    continue
+                self.plan_cache(gamma)
+                try:
+                    gamma = self._iterate(producer, i, gamma, stats, ev)
+                except BaseException:
+                    self.discard_step()
+                    raise
+        finally:
+            torch.cuda.current_stream(self.stream.device).wait_stream(self.stream)
         return stats
 
     def _iterate(self, producer, i: int, gamma: int, stats: LoopStats, ev) -> int:
