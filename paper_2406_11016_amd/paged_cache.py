@@ -351,13 +351,21 @@ class PagedCache:
         self.slots, self.positions = slots, positions
         return slots, positions
 
+    def _described(self, k_cache: torch.Tensor) -> None:
+        """Slots and block tables count in the tables' pages: a cache has such pages, and as many or more."""
+        if k_cache.dim() != 4 or k_cache.shape[2] != self.page_size or k_cache.shape[0] < self.num_pages:
+            raise SpecVerifyError(f"the tables are of {self.num_pages} pages of {self.page_size} tokens; the cache is "
+                                  f"{list(k_cache.shape)}")
+
     def append(self, k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor) -> None:
         """The planned tokens' keys and values ``[B, n, kv_heads, head_dim]`` into their slots."""
+        self._described(k_cache)
         append(k, v, k_cache, v_cache, self.slots)
 
     def append_prefix(self, k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
                       start: int = 0) -> None:
         """Keys and values ``[1, n, kv_heads, head_dim]`` of the prefix's tokens from ``start`` on."""
+        self._described(k_cache)
         end = start + k.shape[1]
         if start < 0 or end > self.prefix_table.numel() * self.page_size:
             raise SpecVerifyError(f"prefix tokens {start} to {end} do not fit {self.prefix_table.numel()} pages")
@@ -378,6 +386,7 @@ class PagedCache:
         and shared by all layers: calls have to be ordered."""
         if q.dim() != 4:
             raise SpecVerifyError(f"q must be [batch, tokens, q_heads, head_dim]; it is {list(q.shape)}")
+        self._described(k_cache)
         key = (q.shape, k_cache.shape[1])
         workspace = self._workspace_of.get(key)
         if workspace is None:
