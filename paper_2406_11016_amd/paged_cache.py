@@ -255,16 +255,19 @@ class PagedCache:
         self._adopt(new(batch), new(batch), new(batch), new(batch, max_pages), new(num_pages), new(1), page_size,
                     max_new)
         self.prefix_table = torch.arange(prefix_pages, dtype=torch.int32, device=self.device)
+        self._prefix_first = True
         self.reset()
 
     @classmethod
     def over(cls, lengths: torch.Tensor, counts: torch.Tensor, held: torch.Tensor, block_table: torch.Tensor,
              free_pages: torch.Tensor, free_count: torch.Tensor, *, page_size: int, max_new: int,
              prefix_table: Optional[torch.Tensor] = None) -> "PagedCache":
-        """Over a program's own tables (int32; see sv_cache_tables_t), as they are."""
+        """Over a program's own tables (int32; see sv_cache_tables_t), as they are.  ``prefix_table`` names the pages
+        of the shared prefix, any that are in no sequence's table and not free."""
         self = cls.__new__(cls)
         self._adopt(lengths, counts, held, block_table, free_pages, free_count, page_size, max_new)
         self.prefix_table = prefix_table if prefix_table is not None else lengths.new_empty(0)
+        self._prefix_first = self.prefix_table.numel() == 0
         _int32("prefix_table", self.prefix_table, (self.prefix_table.numel(),), self._index)
         return self
 
@@ -311,12 +314,21 @@ class PagedCache:
         return got
 
     def reset(self) -> None:
-        """No sequence holds a page; the prefix's pages stay what they are."""
-        _call(self._index, self._lib.spec_cache_init, "spec_cache_init", self._tables_ref, self.prefix_table.numel())
+        """No sequence holds a page, and all pages but the prefix's are free."""
+        _call(self._index, self._lib.spec_cache_init, "spec_cache_init", self._tables_ref,
+              self.prefix_table.numel() if self._prefix_first else 0)
+        if not self._prefix_first:
+            # the prefix's pages, wherever they are, out of the stack
+            page = torch.arange(self.num_pages - 1, -1, -1, dtype=torch.int32, device=self.device)
+            taken = torch.isin(page, self.prefix_table)
+            order = torch.argsort(taken.to(torch.int32), stable=True)
+            self.free_pages.copy_(torch.where(taken[order], -1, page[order]))
+            self.free_count.copy_((~taken).sum())
 
     def set_prefix(self, length: int) -> None:
-        """All sequences begin with the ``length`` tokens in the cache's first pages (token i in slot i).  Graphs
-        captured before go on with the length that was set then."""
+        """All sequences begin with the ``length`` tokens in the prefix's pages (``prefix_table``: the caches' first
+        ones, token i in slot i, unless the program named others).  Graphs captured before go on with the length that
+        was set then."""
         if not 0 <= length <= self.prefix_table.numel() * self.page_size:
             raise SpecVerifyError(f"a prefix of {length} tokens does not fit {self.prefix_table.numel()} pages")
         self.prefix_len = length

@@ -42,3 +42,28 @@ def test_storage_that_the_tables_do_not_describe():
         cache.append_prefix(prefix, prefix, *own)
         cache.append(kv, kv, *own)
         assert not cache.attend(q, *own).any()
+
+
+def _ints(*x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def test_reset_keeps_the_prefix_where_the_program_put_it():
+    """A prefix on pages of the program's choice: reset() hands out all others, in ascending order, and none of those."""
+    N, P, B, M = 12, 16, 3, 4
+    for prefix in ((7, 2), (11,), (0, 1), ()):
+        reserved = _ints(*prefix)
+        cache = PagedCache.over(_ints(*[0] * B), _ints(*[0] * B), _ints(*[0] * B),
+                                torch.full((B, M), -1, dtype=torch.int32, device="cuda"),
+                                torch.empty(N, dtype=torch.int32, device="cuda"), _ints(0), page_size=P, max_new=3 * P,
+                                prefix_table=reserved)
+        for _ in range(2):
+            cache.reset()
+            rest = [p for p in range(N - 1, -1, -1) if p not in prefix]
+            assert int(cache.free_count) == len(rest)
+            assert cache.free_pages.tolist() == rest + [-1] * len(prefix)
+            assert cache.lengths.tolist() == cache.counts.tolist() == cache.held.tolist() == [0] * B
+            assert (cache.block_table == -1).all()
+            cache.plan(3 * P)              # 9 pages, of the 10 or more that there are
+            used = cache.block_table[cache.block_table >= 0].tolist()
+            assert sorted(used) == sorted(rest)[:9] and cache.counts.tolist() == [3 * P] * B
