@@ -146,8 +146,10 @@ sv_status_t spec_cache_append(const sv_cache_append_desc_t* desc, hipStream_t st
  * counts[b] > max_pages * page_size.
  *
  * head_dim is 64, 80, 96, 128 or 256 (for at most SV_CACHE_MAX_BATCH_D256
- * sequences); q_heads a multiple of kv_heads; scale between 1e-30 and 1e30.  Pointers are aligned to 16 bytes, strides (elements; batch,
- * token, head) are multiples of 8.  `workspace` holds
+ * sequences); q_heads a multiple of kv_heads; scale between 1e-30 and 1e30.
+ * Pointers are aligned to 16 bytes, strides (elements; batch, token, head) are
+ * multiples of 8, and out's are not 0 where there is more than one element.
+ * `workspace` holds
  * spec_cache_attend_workspace_bytes() bytes, aligned to 16, and needs no
  * initialisation.
  */

@@ -30,6 +30,11 @@ inline bool strides_ok(const int64_t (&s)[3]) {
     return true;
 }
 
+// A tensor that is written: no two of its rows begin at the same place.
+inline bool rows_apart(const int64_t (&s)[3], int32_t batch, int32_t tokens, int32_t heads) {
+    return (batch == 1 || s[0] != 0) && (tokens == 1 || s[1] != 0) && (heads == 1 || s[2] != 0);
+}
+
 inline bool page_size_ok(int32_t p) { return p >= 16 && p <= 1024 && (p & (p - 1)) == 0; }
 
 inline int32_t page_shift(int32_t p) { return __builtin_ctz((unsigned)p); }
@@ -173,7 +178,8 @@ inline sv_status_t check_attend(const sv_cache_attend_desc_t& d) {
     // (scale * log2(e) and its inverse have to be finite)
     if (!(d.scale > 1e-30f && d.scale < 1e30f)) return SV_ERR_PARAM;
     if (!aligned16(d.q) || !aligned16(d.out) || !aligned16(d.k_cache) || !aligned16(d.v_cache) ||
-        !strides_ok(d.q_stride) || !strides_ok(d.out_stride))
+        !strides_ok(d.q_stride) || !strides_ok(d.out_stride) ||
+        !rows_apart(d.out_stride, d.batch, d.max_new, d.q_heads))
         return SV_ERR_PARAM;
     if (!aligned16(d.workspace) ||
         d.workspace_bytes < attend_workspace_bytes(d.batch, d.max_new, d.q_heads, d.kv_heads, d.head_dim))

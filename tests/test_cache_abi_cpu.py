@@ -214,3 +214,17 @@ def test_device_code_of_every_source(tmp_path):
         kernels += names
     for want in ("verify_kernel", "cache_plan_kernel", "cache_append_kernel", "attend_kernel"):
         assert any(want in k for k in kernels), want
+
+
+def test_outputs_that_overlap_themselves_are_refused(lib):
+    """Rows of the output that lie on one another (an expanded view) would be written by several workgroups at once;
+    dimensions of one element may have any stride, and q may be expanded (it is only read)."""
+    for i in range(3):
+        strides = [1536, 512, 128]
+        strides[i] = 0
+        assert _attend(lib, out_stride=tuple(strides)) == PARAM, i
+        # (up to here; no call may reach the GPU)
+        assert _attend(lib, q_stride=tuple(strides), workspace_bytes=0) == WORKSPACE, i
+    assert _attend(lib, batch=1, out_stride=(0, 512, 128), workspace_bytes=0) == WORKSPACE
+    assert _attend(lib, max_new=1, out_stride=(512, 0, 128), workspace_bytes=0) == WORKSPACE
+    assert _attend(lib, q_heads=1, kv_heads=1, out_stride=(1536, 512, 0), workspace_bytes=0) == WORKSPACE
