@@ -112,8 +112,8 @@ class DecodeLoop:
         self.gamma0, self.gamma_max, self.use_graphs = gamma0, gamma_max, use_graphs
         self.device = torch.device(device)
         if cache is not None and (cache.batch != batch or cache.max_new < gamma_max + 1 or
-                                  cache.device.type != self.device.type or
-                                  self.device.index not in (None, cache.device.index)):
+                                  cache.device.type != self.device.type or cache.device.index !=
+                                  (torch.cuda.current_device() if self.device.index is None else self.device.index)):
             raise ValueError(f"the cache must serve {batch} sequences and {gamma_max + 1} new tokens on {self.device}; "
                              f"it has {cache.batch}, {cache.max_new} on {cache.device}")
         self.cache = cache

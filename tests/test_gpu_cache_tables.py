@@ -6,6 +6,7 @@ import torch
 
 from paper_2406_11016_amd import paged_cache
 from paper_2406_11016_amd.binding import SpecVerifyError
+from paper_2406_11016_amd.decode_loop import DecodeLoop
 from paper_2406_11016_amd.paged_cache import PagedCache
 
 pytestmark = pytest.mark.gpu
@@ -67,3 +68,12 @@ def test_reset_keeps_the_prefix_where_the_program_put_it():
             cache.plan(3 * P)              # 9 pages, of the 10 or more that there are
             used = cache.block_table[cache.block_table >= 0].tolist()
             assert sorted(used) == sorted(rest)[:9] and cache.counts.tolist() == [3 * P] * B
+
+
+def test_a_loop_on_another_device_than_its_cache():
+    class Other:
+        batch, max_new, device = 2, 5, torch.device("cuda", torch.cuda.current_device() + 1)
+
+    for device in ("cuda", f"cuda:{torch.cuda.current_device()}"):
+        with pytest.raises(ValueError, match="the cache must serve"):
+            DecodeLoop(2, 100, "f32", gamma0=1, gamma_max=4, cache=Other(), device=device)
