@@ -50,7 +50,7 @@ struct AttendArgs {
     uint32_t* cum_cost;   // [batch + 1] cost of the own tasks before each sequence's
     float* part_out;      // parts: rows x head_dim, fp32
     Totals* totals;       // of the split
-    float* part_max;      // maximum (scores in log2 units)
+    float* part_max;      // maximum (scores as they come from the product)
     float* part_sum;
 };
 
@@ -94,6 +94,12 @@ struct AttBF16 {
 
 constexpr int kThreads = 256;
 constexpr int kKeys = kAttendKeys;
+
+// Scores, in log2 units, up to which a weight's argument is taken in one fused
+// multiply-add, score * scale - reference: the reference there is a product rounded to 32
+// bits, so all weights of a row are off by one common factor, 2^(2^-12) at most.  Behind it the factor
+// would not fit the weights' type in the end, and a score loses its reference first.
+constexpr float kFarScores = 4096.0f;
 
 // A value that is the same in every lane, in a scalar register.
 __device__ __forceinline__ int32_t uniform(int32_t x) { return __builtin_amdgcn_readfirstlane(x); }
@@ -503,6 +509,7 @@ __device__ __forceinline__ bool segment(Work<D, kKind>& work, char* smem, float 
     }
     f32x16 o[kPieces];
     float top, sum = 0.0f;  // top: scores as they come from the product
+    bool far;               // some row's is beyond kFarScores: the scores of the unit at hand have lost it already
 
     // Places of this lane's reads.  The swizzle flips bits of the chunk's number
     // only, so a read's constant part comes by an exclusive or (chunk) or as an
@@ -540,6 +547,16 @@ __device__ __forceinline__ bool segment(Work<D, kKind>& work, char* smem, float 
             }
         return most;
     };
+    // Whether, and then the scores without it.
+    auto look_far = [&]() {
+        far = __any(fabsf(top * a.scale_log2) > kFarScores && top != -INFINITY);
+    };
+    auto take_off = [&](f32x16(&p)[NS]) {
+        if (!far) return;
+        const float ref = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+        for (int s = 0; s < NS; ++s) p[s] -= ref;
+    };
     // Moves the reference of the weights to unit u's maximum: they stay relative to a maximum of earlier units as
     // long as the new one is within 2^8 of it, so nothing is rescaled for small rises.
     auto refer = [&](auto full, uint32_t u, f32x16(&p)[NS], float most) {
@@ -552,7 +569,9 @@ __device__ __forceinline__ bool segment(Work<D, kKind>& work, char* smem, float 
 #pragma unroll
             for (int i = 0; i < kPieces; ++i) o[i] *= by;
             top = now;
+            look_far();
         }
+        take_off(p);
     };
     // One unit: p's scores are masked and referred to; `next` gets the scores of the unit after it.  The segment's
     // even units lie in the first two tiles of LDS (K, V), its odd ones in the others.  `full`: it and the two units
@@ -563,7 +582,7 @@ __device__ __forceinline__ bool segment(Work<D, kKind>& work, char* smem, float 
         constexpr int kHere = decltype(odd)::value * S::kStage, kThere = S::kStage - kHere;
         const bool more = kFull || u + 1 < g.end;
         char* const v_tile = smem + kHere + S::kTile;
-        float shift = (top == -INFINITY) ? 0.0f : -top * a.scale_log2;
+        float shift = (far || top == -INFINITY) ? 0.0f : -top * a.scale_log2;
         float add = 0.0f;
         auto weigh = [&](int from, int to) {
 #pragma unroll
@@ -690,6 +709,8 @@ __device__ __forceinline__ bool segment(Work<D, kKind>& work, char* smem, float 
             for (int i = 0; i < 16; ++i) most = fmaxf(most, scores[0][s][i]);
         if (partial_of(g.first)) most = mask(g.first, scores[0]);
         top = halves_max(most);
+        look_far();
+        take_off(scores[0]);
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) o[i] = f32x16(0.0f);
     }
@@ -722,8 +743,8 @@ __device__ __forceinline__ bool segment(Work<D, kKind>& work, char* smem, float 
             const float(*const other)[32] = wave_stats[wave + (wk == 0 ? WR : -WR)];
             const float other_top = other[0][lane & 31], now = fmaxf(top, other_top);
             const float ref = (now == -INFINITY) ? 0.0f : now;
-            const float by = exp2_hw(top - ref);
-            const float own = by * sum, others = exp2_hw(other_top - ref) * other[1][lane & 31];
+            const float by = exp2_hw((top - ref) * a.scale_log2);
+            const float own = by * sum, others = exp2_hw((other_top - ref) * a.scale_log2) * other[1][lane & 31];
             sum = wk == 0 ? own + others : others + own;
             top = now;
             // piece i of the output is summed by the wave wk = i % WK
@@ -791,7 +812,6 @@ __device__ __forceinline__ bool segment(Work<D, kKind>& work, char* smem, float 
         }
     };
     sum = halves_sum(sum);
-    top *= a.scale_log2;
     if (work.poison) *poison_flag = 1;
     const bool whole = kKind == kJoined && work.whole;
     const int64_t place = work.place;
@@ -916,7 +936,8 @@ struct Joiner {
 #pragma unroll
                 for (int m = 1; m < 64; m <<= 1) now = fmaxf(now, __shfl_xor(now, m));
                 const float ref = now == -INFINITY ? 0.0f : now;
-                const float before = exp2_hw(top - ref), by = lane < count ? exp2_hw(most - ref) : 0.0f;
+                const float before = exp2_hw((top - ref) * a.scale_log2);
+                const float by = lane < count ? exp2_hw((most - ref) * a.scale_log2) : 0.0f;
                 sum = before * sum + by * part_sum;
                 out *= before;
                 top = now;
@@ -978,7 +999,7 @@ __device__ __forceinline__ void join_by_block(const AttendArgs& a, int n, Place 
         own.out = f32x4(0.0f);
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) {
-            const float by = exp2_hw(box[w][D] - ref);
+            const float by = exp2_hw((box[w][D] - ref) * a.scale_log2);
             own.sum += by * box[w][D + 1];
             own.out += by * *(const f32x4*)&box[w][own.d];
         }
@@ -1062,7 +1083,7 @@ __device__ __forceinline__ void join_two(const AttendArgs& a, int64_t first, int
     for (int i = 0; i < kEach; ++i) {
         if (to[i] == nullptr) continue;
         const float top = fmaxf(most[i][0], most[i][1]), ref = top == -INFINITY ? 0.0f : top;
-        const float w0 = exp2_hw(most[i][0] - ref), w1 = exp2_hw(most[i][1] - ref);
+        const float w0 = exp2_hw((most[i][0] - ref) * a.scale_log2), w1 = exp2_hw((most[i][1] - ref) * a.scale_log2);
         f32x4 all = w0 * x[i][0];
         all += w1 * x[i][1];
         all *= 1.0f / (w0 * sum[i][0] + w1 * sum[i][1]);

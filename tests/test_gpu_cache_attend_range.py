@@ -1,0 +1,115 @@
+"""The cache's attention at the ends of its types' ranges: scores far from zero."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2406_11016_amd import paged_cache
+from tests.cache_util import TORCH_DTYPES
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def gpu():
+    if not torch.cuda.is_available():
+        pytest.fail("no GPU visible")
+    paged_cache.load_library()
+    torch.cuda.init()
+
+
+def _batch(n, H, D, P, prefix, lengths, dtype, seed):
+    """Random values; keys that only have entries 0 and 1, set by the caller through `place`."""
+    t = TORCH_DTYPES[dtype]
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    B, M, shared = len(lengths), -(-(max(lengths) + n) // P), -(-prefix // P)
+    order = torch.randperm(B * M + shared, generator=gen, device="cuda").to(torch.int32)
+    table, prefix_table = order[:B * M].view(B, M), order[B * M:].contiguous()
+    k = torch.zeros(B * M + shared, 1, P, D, dtype=t, device="cuda")
+    v = torch.randn(B * M + shared, 1, P, D, generator=gen, device="cuda").to(t)
+    q = torch.zeros(B, n, H, D, dtype=t, device="cuda")
+
+    def place(b, j):
+        """Pages and places of tokens j (a tensor) of sequence b, the prefix's first."""
+        own = j - prefix
+        pages = torch.where(own >= 0, table[b][(own.clamp(min=0) // P)],
+                            prefix_table[(j // P).clamp(max=max(shared - 1, 0))] if shared else table[b][0])
+        return pages.long(), torch.where(own >= 0, own, j) % P
+
+    return q, k, v, table.contiguous(), prefix_table, place
+
+
+# a score is scale times a small whole number, so it is exact in 32 bits, and other keys are at least `scale` behind
+SCALES = [2.0 ** 6, 2.0 ** 13, 2.0 ** 24, 2.0 ** 27, 2.0 ** 40, 2.0 ** 96, 9e29]
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("n,D,P,prefix,lengths", [(1, 64, 16, 0, [20000]), (3, 128, 16, 150, [300, 0]),
+                                                  (9, 80, 32, 0, [700, 5, 64]), (2, 256, 64, 4000, [900]),
+                                                  (40, 128, 64, 0, [500, 200])], ids=str)
+def test_far_scores_choose_the_nearest_key(n, D, P, prefix, lengths, dtype):
+    """Softmax weights at such scales are 1 / (number of keys with the highest score), and 0 elsewhere.
+
+    Of four heads one looks for the highest number, one for the lowest, one for the highest with scores below zero and
+    one has all scores 0.  The bound counts the rounding of the weights and of the output, u each, the sums of a few
+    equal weights in fp32 and, where all keys count, those of all of them.
+    """
+    H, t = 4, TORCH_DTYPES[dtype]
+    u = torch.finfo(t).eps / 2
+    for scale in SCALES:
+        q, k, v, table, prefix_table, place = _batch(n, H, D, P, prefix, lengths, dtype, seed=n)
+        rng = np.random.default_rng(n)
+        q[:, :, 0, 0] = 1.0
+        q[:, :, 1, 0] = -1.0
+        q[:, :, 2, 0], q[:, :, 2, 1] = 2.0, -1.0
+        numbers = rng.integers(-60, 61, max(prefix, 1))
+        expect = torch.empty(len(lengths), n, H, D, dtype=torch.float64)
+        most = torch.empty(len(lengths), n, H, dtype=torch.float64)
+        for b, length in enumerate(lengths):
+            every = np.concatenate([numbers[:prefix], rng.integers(-60, 61, length + n)])
+            j = torch.arange(len(every), device="cuda")
+            pages, at = place(b, j)
+            k[pages, 0, at, 0] = torch.tensor(every, device="cuda").to(t)
+            k[pages, 0, at, 1] = 240.0
+            values = v[pages, 0, at].double().cpu()
+            for i in range(n):
+                seen = every[:prefix + length + i + 1]
+                for h, score in enumerate((seen, -seen, 2 * seen - 240, 0 * seen)):
+                    best = np.flatnonzero(score == score.max())
+                    expect[b, i, h] = values[best].mean(0)
+                    most[b, i, h] = values[best].abs().mean(0).max()
+                    if h < 3:          # 1 + the others' weights, at most exp(-64) each
+                        assert (np.sort(score)[-len(best) - 1] < score.max() if len(best) < len(score) else True)
+        out = paged_cache.attend(q, k, v, table, torch.tensor(lengths, dtype=torch.int32, device="cuda"),
+                                 prefix_table=prefix_table, prefix_len=prefix, scale=scale).double().cpu()
+        keys = prefix + max(lengths) + n
+        bound = (2 * u * (1 + u) + 2 * (keys + 64) * 2.0 ** -24) * most[..., None] + \
+            (2.0 ** -24 if dtype == "f16" else 0.0)
+        wrong = ~((out - expect).abs() <= bound)
+        assert not wrong.any(), (scale, wrong.nonzero()[:4].tolist(), out[wrong][:4], expect[wrong][:4])
+
+
+@pytest.mark.parametrize("dtype,large", [("f16", 60000.0), ("bf16", 1e17)])
+@pytest.mark.parametrize("prefix", [0, 130])
+def test_scores_whose_product_with_the_scale_is_past_32_bits(dtype, large, prefix):
+    """Scores of q k up to 1e9 (fp16) and 1e34 (bf16), times a scale with which they pass the largest fp32 number."""
+    lengths, n, D = [400, 70], 3, 64
+    scale = 9e29 if dtype == "f16" else 1e6
+    t = TORCH_DTYPES[dtype]
+    q, k, v, table, prefix_table, place = _batch(n, 2, D, 16, prefix, lengths, dtype, seed=4)
+    q[:, :, 0, 0], q[:, :, 1, 0] = large, -large
+    for b, length in enumerate(lengths):
+        j = torch.arange(prefix + length + n, device="cuda")
+        pages, at = place(b, j)
+        k[pages, 0, at, 0] = ((j * 37 % 101).float() * (large / 128)).to(t)
+    out = paged_cache.attend(q, k, v, table, torch.tensor(lengths, dtype=torch.int32, device="cuda"),
+                             prefix_table=prefix_table, prefix_len=prefix, scale=scale)
+    u = torch.finfo(t).eps / 2
+    for b, length in enumerate(lengths):
+        for i in range(n):
+            j = torch.arange(prefix + length + i + 1, device="cuda")
+            pages, at = place(b, j)
+            key = k[pages, 0, at, 0].double()
+            for h, best in enumerate((key == key.max(), key == key.min())):
+                values = v[pages, 0, at][best].double()
+                bound = (2 * u * (1 + u) + 600 * 2.0 ** -23) * values.abs().mean(0).max() + 2.0 ** -24
+                assert ((out[b, i, h].double() - values.mean(0)).abs() <= bound).all(), (b, i, h)
