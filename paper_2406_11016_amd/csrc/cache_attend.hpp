@@ -71,7 +71,11 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 #define SV_LDS __attribute__((address_space(3)))
 
+// kBias: the largest weight of a row in log2, but for rises of the maximum that are let pass (up to 8).
 struct AttF16 {
+    // 2^15 is the largest power of two in fp16, so weights down to 2^-31 of the largest are
+    // not lost to 0 (2^-24 without it)
+    static constexpr float kBias = 7.0f;
     typedef _Float16 V8 __attribute__((ext_vector_type(8)));
     typedef _Float16 V4 __attribute__((ext_vector_type(4)));
     static __device__ __forceinline__ f32x16 mma(V8 a, V8 b, f32x16 c) {
@@ -83,6 +87,7 @@ struct AttF16 {
     }
 };
 struct AttBF16 {
+    static constexpr float kBias = 0.0f;
     typedef __bf16 V8 __attribute__((ext_vector_type(8)));
     typedef __bf16 V4 __attribute__((ext_vector_type(4)));
     static __device__ __forceinline__ f32x16 mma(V8 a, V8 b, f32x16 c) {
@@ -582,7 +587,7 @@ __device__ __forceinline__ bool segment(Work<D, kKind>& work, char* smem, float 
         constexpr int kHere = decltype(odd)::value * S::kStage, kThere = S::kStage - kHere;
         const bool more = kFull || u + 1 < g.end;
         char* const v_tile = smem + kHere + S::kTile;
-        float shift = (far || top == -INFINITY) ? 0.0f : -top * a.scale_log2;
+        float shift = (far || top == -INFINITY) ? T::kBias : fmaf(-top, a.scale_log2, T::kBias);
         float add = 0.0f;
         auto weigh = [&](int from, int to) {
 #pragma unroll

@@ -113,3 +113,31 @@ def test_scores_whose_product_with_the_scale_is_past_32_bits(dtype, large, prefi
                 values = v[pages, 0, at][best].double()
                 bound = (2 * u * (1 + u) + 600 * 2.0 ** -23) * values.abs().mean(0).max() + 2.0 ** -24
                 assert ((out[b, i, h].double() - values.mean(0)).abs() <= bound).all(), (b, i, h)
+
+
+@pytest.mark.parametrize("prefix", [0, 1000])
+def test_small_fp16_weights_of_large_values_count(prefix):
+    """One key of value 0 and a thousand others of weight 2^-26 and 2^-28, below half of what fp16 holds next to 1.
+
+    600 sequences share the pages, so a workgroup has each sequence's keys whole but for the borders.  The bound: the
+    output rounded, u; scores exact; 2 (keys + 64) roundings of 2^-24 of the sums; and the weights rounded: these are
+    numbers below 2^-14, whose steps are 2^-24, next to a largest one of 2^7, so off by 2^-32 of that each.
+    """
+    D, P, B, own = 64, 64, 600, 0 if prefix else 1000
+    q, k, v, table, prefix_table, place = _batch(1, 1, D, P, prefix, [own] * B, "f16", seed=1)
+    table[:] = table[0]
+    q[:, :, 0, 0] = 1.0
+    j = torch.arange(1001, device="cuda")
+    pages, at = place(0, j)
+    score = torch.where(j % 2 == 0, -18.02, -19.41).to(torch.float16)     # 2^-26, 2^-28
+    values = torch.randint(1, 60, (1001, D), device="cuda", generator=torch.Generator(device="cuda").manual_seed(3)) * 1000
+    values = values.to(torch.float16)
+    score[500], values[500] = 0.0, 0.0
+    score[1000], values[1000] = -30.0, 0.0                                # (the new token)
+    k[pages, 0, at, 0], v[pages, 0, at] = score, values
+    out = paged_cache.attend(q, k, v, table, torch.full((B,), own, dtype=torch.int32, device="cuda"),
+                             prefix_table=prefix_table, prefix_len=prefix, scale=1.0).double()
+    want = torch.softmax(score.double(), 0) @ values.double()
+    assert float(want.min()) > 0.1
+    bound = (2.0 ** -11 + 2 * 1065 * 2.0 ** -24) * want + 2.0 ** -32 * values.double().sum(0)
+    assert ((out[:, 0, 0] - want).abs() <= bound).all(), (out[0, 0, 0, :4], want[:4])
