@@ -87,7 +87,10 @@ struct AttF16 {
     }
 };
 struct AttBF16 {
-    static constexpr float kBias = 0.0f;
+    // bf16 holds numbers up to fp32's largest, 2^128: so the sums of 2^20 largest weights (2^8 more
+    // for the time being) and any finite values are finite, and what is lost at the other end are products
+    // below 2^-98 (2^-126 without it)
+    static constexpr float kBias = -28.0f;
     typedef __bf16 V8 __attribute__((ext_vector_type(8)));
     typedef __bf16 V4 __attribute__((ext_vector_type(4)));
     static __device__ __forceinline__ f32x16 mma(V8 a, V8 b, f32x16 c) {

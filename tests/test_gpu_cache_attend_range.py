@@ -141,3 +141,39 @@ def test_small_fp16_weights_of_large_values_count(prefix):
     assert float(want.min()) > 0.1
     bound = (2.0 ** -11 + 2 * 1065 * 2.0 ** -24) * want + 2.0 ** -32 * values.double().sum(0)
     assert ((out[:, 0, 0] - want).abs() <= bound).all(), (out[0, 0, 0, :4], want[:4])
+
+@pytest.mark.parametrize("prefix", [0, 300])
+@pytest.mark.parametrize("n,D", [(1, 64), (6, 128), (30, 128)])
+def test_large_values_do_not_overflow(n, D, prefix):
+    """bfloat16 values near the type's largest number, all of one sign or of both, under scores that rise: weights that
+    are larger than 1 for the time being, and sums of many of them, stay finite.
+
+    The definition's result is at most the largest |v|; the bound is the rounding of weights and output (u each, of the
+    sum of w |v|, which is at most 1.1e38 here) and 2 (keys + 64) roundings of 2^-24.
+    """
+    lengths = [900, 20]
+    q, k, v, table, prefix_table, place = _batch(n, 2, D, 16, prefix, lengths, "bf16", seed=2)
+    q[:, :, :, 0] = 1.0
+    q[:, :, 1, 1] = 1.0
+    for b, length in enumerate(lengths):
+        j = torch.arange(prefix + length + n, device="cuda")
+        pages, at = place(b, j)
+        k[pages, 0, at, 0] = ((j // 64) % 6).to(torch.bfloat16)            # up to 5, 7.2 in log2 units
+        k[pages, 0, at, 1] = -((j // 64) % 6).to(torch.bfloat16)           # (head 1: all weights alike)
+        v[pages, 0, at] = 1e38
+        v[pages, 0, at, 1] = torch.where(j % 2 == 0, 1.1e38, -1e38).to(torch.bfloat16)
+        v[pages, 0, at, 2] = 1.0
+    out = paged_cache.attend(q, k, v, table, torch.tensor(lengths, dtype=torch.int32, device="cuda"),
+                             prefix_table=prefix_table, prefix_len=prefix, scale=1.0).double().cpu()
+    u = 2.0 ** -8
+    for b, length in enumerate(lengths):
+        for i in range(n):
+            j = torch.arange(prefix + length + i + 1, device="cuda")
+            pages, at = place(b, j)
+            for h in range(2):
+                z = k[pages, 0, at].double() @ q[b, i, h].double()
+                w = torch.softmax(z, 0)
+                values = v[pages, 0, at].double()
+                want, size = (w @ values).cpu(), (w @ values.abs()).cpu()
+                bound = (2 * u * (1 + u) + 2 * (len(j) + 64) * 2.0 ** -24) * size
+                assert ((out[b, i, h] - want).abs() <= bound).all(), (b, i, h, out[b, i, h, :3], want[:3])
