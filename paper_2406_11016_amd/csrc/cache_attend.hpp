@@ -379,7 +379,17 @@ struct Work {
         poison = g.bad;
         paged = g.first;
         look_up();
+        if constexpr (kKind != kShared) look_behind();
         return true;
+    }
+    // A sequence with a page that there is not has no outputs: pages that only later row tiles need.
+    __device__ __forceinline__ void look_behind() {
+        const int end = own_end(a.split, g), last = g.length + g.count - 1;
+        if (g.bad || end > last) return;
+        const int32_t* const table = a.block_table + (int64_t)g.b * a.split.max_pages;
+        for (int j = ((end - 1) >> a.split.page_shift) + 1 + forget((int)threadIdx.x); j <= last >> a.split.page_shift;
+             j += kThreads)
+            if ((uint32_t)table[j] >= (uint32_t)a.num_pages) poison = true;
     }
     // Whether unit u is of the prefix, its first key there or in the sequence, and the last key that there is.
     __device__ __forceinline__ bool in_prefix(uint32_t u) const {
