@@ -130,15 +130,18 @@ sv_status_t spec_cache_append(const sv_cache_append_desc_t* desc, hipStream_t st
  *
  *   out[b, i, h] = sum_j w_j v_j / sum_j w_j,   w_j = exp(scale q[b, i, h] . k_j)
  *
- * with the keys and values of head h / (q_heads / kv_heads).  The shared prefix
- * is read once for the batch.  q and out [batch, max_new, q_heads, head_dim] do
- * not overlap;
+ * with the keys and values of head h / (q_heads / kv_heads).  The tokens of the
+ * whole batch share the reads of the prefix: it is read for tiles of up to 128
+ * rows (token x head), not for sequences, and by neighbouring tiles through one
+ * cache.  q and out [batch, max_new, q_heads, head_dim] do not overlap;
  * rows behind counts[b] are neither read nor written (all of them where
  * counts[b] <= 0; without `counts` every sequence has max_new).  Entries of the
  * cache that a token does not see have no influence on it, whatever their bits.
  *
- * Statistics and sums are held in fp32; the weights are rounded to the storage
- * type for their product with the values, relative to a maximum.
+ * Scores, statistics and sums are held in fp32; the weights are rounded to the
+ * storage type for their product with the values (what is rounded off would take a
+ * second product).  Weights below 2^-31 (fp16) or 2^-98 (bf16) of a row's largest
+ * may count as 0 there, so an infinite value of such a key gives infinity or NaN.
  *
  * Bad data found on the device makes the outputs of the sequence NaN: a page
  * outside 0 .. num_pages - 1 among those that the sequence needs (in the prefix:
