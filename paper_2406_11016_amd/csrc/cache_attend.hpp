@@ -465,8 +465,10 @@ struct Work {
 // the registers of two lanes (l and l + 32), so the maximum and the sum over the
 // keys need one exchange between lanes, and the running maximum, the sum and the
 // rescaling of the output are one value a lane.  P^T then is the B operand of
-// O^T = V^T P^T as it stands (after rounding to the storage type), with V^T from
-// LDS by transposing reads in the same order of keys.
+// O^T = V^T P^T as it stands, with V^T from LDS by transposing reads in the same order
+// of keys.  It is rounded to the storage type for that, half a step a weight: what is
+// rounded off would be a second product, half of a unit's matrix instructions again.
+// (The sum of the weights is of the unrounded ones.)
 //
 // K runs one unit ahead of V: while one unit's scores become weights, on the
 // vector units, the matrix units make the next one's scores, product by product in

@@ -13,8 +13,8 @@ This module has the cache's operators, each a call of the HIP library
 * :func:`append` (:meth:`PagedCache.append`) writes new keys and values to the
   mapped slots;
 * :func:`attend` (:meth:`PagedCache.attend`) is the attention of the new tokens
-  to a prefix that the whole batch shares, read once for all of it, and to each
-  sequence's own entries.
+  to a prefix that the whole batch shares, whose reads the sequences' tokens
+  share, and to each sequence's own entries.
 
 A step of a target model with such a cache::
 
@@ -197,8 +197,9 @@ def attend(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, block_
 
     Token i of sequence b sees the shared prefix (``prefix_len`` tokens in the pages of ``prefix_table``, int32) and
     its sequence's own tokens ``0 .. lengths[b] + i`` (``block_table [B, max_pages]``, ``lengths [B]``, int32).  Rows
-    behind ``counts[b]`` (int32 [B]; all n without it) are neither read nor written; a new ``out`` is zero there.
-    ``out`` does not overlap ``q``.  At head_dim 256 the batch is at most 2,048, else 4,096.  ``scale`` (1e-30 to 1e30)
+    behind ``counts[b]`` (int32 [B]; all n without it) are neither read nor written; a new ``out`` is zero there, for
+    which all of it is filled first: pass ``out`` to go without.  ``out`` does not overlap ``q``, nor itself.  For
+    inference: the result has no gradient, whatever ``q`` requires.  At head_dim 256 the batch is at most 2,048, else 4,096.  ``scale`` (1e-30 to 1e30)
     defaults to ``head_dim ** -0.5``.  ``workspace`` (see new_attend_workspace) avoids an allocation a call.
     """
     lib = _lib if _lib is not None else load_library()
@@ -241,7 +242,8 @@ class PagedCache:
 
     ``num_pages`` pages of ``page_size`` tokens (a power of two from 16 to 1024) serve ``batch`` sequences of up to
     ``max_pages`` pages each and, in the first ``prefix_pages`` of them, a prefix that all sequences share
-    (:meth:`set_prefix`).  The buffers are static: captured graphs may hold them.
+    (:meth:`set_prefix`).  The buffers are static: captured graphs may hold them.  Calls go to the current stream and
+    have to be ordered, as all calls that share tables, caches or a workspace.
     """
 
     def __init__(self, batch: int, *, num_pages: int, page_size: int, max_pages: int, max_new: int,
