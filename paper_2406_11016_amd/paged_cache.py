@@ -316,7 +316,10 @@ class PagedCache:
         return got
 
     def reset(self) -> None:
-        """No sequence holds a page, and all pages but the prefix's are free."""
+        """No sequence holds a page, and all pages but the prefix's are free.  (With a prefix on pages of the program's
+        choice not in a captured graph: sorting the pages clears memory in ways that replays do not repeat.)"""
+        if not self._prefix_first and torch.cuda.is_current_stream_capturing():
+            raise SpecVerifyError("reset() with a prefix on pages of the program's choice cannot be captured")
         _call(self._index, self._lib.spec_cache_init, "spec_cache_init", self._tables_ref,
               self.prefix_table.numel() if self._prefix_first else 0)
         if not self._prefix_first:

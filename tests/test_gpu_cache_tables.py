@@ -77,3 +77,35 @@ def test_a_loop_on_another_device_than_its_cache():
     for device in ("cuda", f"cuda:{torch.cuda.current_device()}"):
         with pytest.raises(ValueError, match="the cache must serve"):
             DecodeLoop(2, 100, "f32", gamma0=1, gamma_max=4, cache=Other(), device=device)
+
+
+def test_reset_in_a_graph():
+    """Of the tables' own order; a prefix on pages of the program's choice is refused there."""
+    tables = [torch.zeros(2, dtype=torch.int32, device="cuda") for _ in range(3)]
+    rows, free = torch.zeros(2, 3, dtype=torch.int32, device="cuda"), torch.zeros(9, dtype=torch.int32, device="cuda")
+    kinds = {}
+    for name, prefix in (("none", None), ("chosen", _ints(4, 2))):
+        kinds[name] = PagedCache.over(*tables, rows, free, _ints(0), page_size=16, max_new=4, prefix_table=prefix)
+    kinds["first"] = PagedCache(2, num_pages=9, page_size=16, max_pages=3, max_new=4, prefix_pages=2)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for name in ("none", "first"):
+        cache = kinds[name]
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            cache.reset()
+        for _ in range(3):
+            cache.plan(4)
+            torch.cuda.synchronize()
+            g.replay()
+            torch.cuda.synchronize()
+            first = cache.prefix_table.numel()
+            assert int(cache.free_count) == 9 - first
+            assert cache.free_pages.tolist() == list(range(8, first - 1, -1)) + [-1] * first
+    with torch.cuda.stream(side):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            with pytest.raises(SpecVerifyError, match="captured"):
+                kinds["chosen"].reset()
+            kinds["none"].reset()
+    torch.cuda.synchronize()
