@@ -582,7 +582,8 @@ __device__ __forceinline__ bool segment(Work<D, kKind>& work, char* smem, float 
     auto refer = [&](auto full, uint32_t u, f32x16(&p)[NS], float most) {
         if (!decltype(full)::value && partial_of(u)) most = mask(u, p);
         most = halves_max(most);
-        if (__any(most > top + a.lazy)) {
+        // (the difference of two scores near one another is exact; next to a far one a.lazy would be rounded)
+        if (__any(most - top > a.lazy)) {
             const float now = fmaxf(top, most);
             const float by = (now == -INFINITY) ? 1.0f : exp2_hw((top - now) * a.scale_log2);
             sum *= by;

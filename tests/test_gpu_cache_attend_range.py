@@ -177,3 +177,38 @@ def test_large_values_do_not_overflow(n, D, prefix):
                 want, size = (w @ values).cpu(), (w @ values.abs()).cpu()
                 bound = (2 * u * (1 + u) + 2 * (len(j) + 64) * 2.0 ** -24) * size
                 assert ((out[b, i, h] - want).abs() <= bound).all(), (b, i, h, out[b, i, h, :3], want[:3])
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("prefix", [0, 130])
+@pytest.mark.parametrize("steps", [1.0, 3.0, 6.0, 12.0])
+def test_rises_of_the_last_bit_of_far_scores(dtype, prefix, steps):
+    """Scores 4096 + j 2^-11, exact in fp32, one last bit apart, which is `steps` in log2 units: what a rise that is let
+    pass may be is found from the difference, not next to the score, where it would be rounded to whole bits.
+
+    Bound: as in attend_bound with exact scores; a weight's argument (at most 5 steps, 60) is off by 4 roundings of
+    2^-24, scale's among them, so the weights by 2^-16 of themselves, twice.
+    """
+    n, D, B, length = 2, 64, 600, 400      # (of one set of pages: a workgroup has most of a sequence's units)
+    q, k, v, table, prefix_table, place = _batch(n, 2, D, 16, prefix, [length] * B, dtype, seed=9)
+    table[:] = table[0]
+    q[:, :, :, 0], q[:, :, :, 1] = 64.0, 2.0 ** -11
+    scale = steps * 2.0 ** 11 * float(np.log(2.0))
+    want, size = (torch.empty(n, 2, D, dtype=torch.float64, device="cuda") for _ in range(2))
+    j = torch.arange(prefix + length + n, device="cuda")
+    pages, at = place(0, j)
+    k[pages, 0, at, 0] = 64.0
+    k[pages, 0, at, 1] = ((j // 64) % 6).to(k.dtype)       # (a unit of keys after the other)
+    for i in range(n):
+        seen = slice(0, prefix + length + i + 1)
+        z = k[pages[seen], 0, at[seen]].double() @ q[0, i].double().t()
+        w = torch.softmax(z * float(np.float32(scale)), 0)
+        values = v[pages[seen], 0, at[seen]].double()
+        want[i], size[i] = w.t() @ values, w.t() @ values.abs()
+    out = paged_cache.attend(q, k, v, table, torch.full((B,), length, dtype=torch.int32, device="cuda"),
+                             prefix_table=prefix_table, prefix_len=prefix, scale=scale).double()
+    u, keys = torch.finfo(TORCH_DTYPES[dtype]).eps / 2, prefix + 402
+    bound = (2 * u * (1 + u) + 2 * 2.0 ** -16 + 2 * (keys + 64) * 2.0 ** -24) * size + \
+        (keys * 2.0 ** -32 * 5.0 + 2.0 ** -25 if dtype == "f16" else 0.0)
+    wrong = ~((out - want).abs() <= bound)
+    assert not wrong.any(), (wrong.nonzero()[:3].tolist(), out[wrong][:4], want.expand_as(out)[wrong][:4])
