@@ -141,7 +141,8 @@ sv_status_t spec_cache_append(const sv_cache_append_desc_t* desc, hipStream_t st
  * Scores, statistics and sums are held in fp32; the weights are rounded to the
  * storage type for their product with the values (what is rounded off would take a
  * second product).  Weights below 2^-31 (fp16) or 2^-98 (bf16) of a row's largest
- * may count as 0 there, so an infinite value of such a key gives infinity or NaN.
+ * may count as 0 there, so an infinite value of such a key gives infinity or NaN;
+ * so may, in bf16, products of such a relative weight and a value below 2^-98.
  *
  * Bad data found on the device makes the outputs of the sequence NaN: a page
  * outside 0 .. num_pages - 1 among those that the sequence needs (in the prefix:

@@ -281,7 +281,9 @@ class DecodeLoop:
             time_device: bool = False) -> LoopStats:
         """``iterations`` rounds of: producer(self, i, gamma) fills the buffers
         (on ``self.stream``), the step runs, gamma is updated.  With
-        ``time_device`` each step is bracketed by HIP events on the stream."""
+        ``time_device`` each step is bracketed by HIP events on the stream.
+        ``stats`` of the caller's own has the completed iterations also where
+        one raises."""
         stats = stats or LoopStats()
         gamma = self.gamma0
         ev = (torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)) if time_device else None

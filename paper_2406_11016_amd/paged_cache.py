@@ -199,8 +199,9 @@ def attend(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, block_
     its sequence's own tokens ``0 .. lengths[b] + i`` (``block_table [B, max_pages]``, ``lengths [B]``, int32).  Rows
     behind ``counts[b]`` (int32 [B]; all n without it) are neither read nor written; a new ``out`` is zero there, for
     which all of it is filled first: pass ``out`` to go without.  ``out`` does not overlap ``q``, nor itself.  For
-    inference: the result has no gradient, whatever ``q`` requires.  At head_dim 256 the batch is at most 2,048, else 4,096.  ``scale`` (1e-30 to 1e30)
-    defaults to ``head_dim ** -0.5``.  ``workspace`` (see new_attend_workspace) avoids an allocation a call.
+    inference: the result has no gradient, whatever ``q`` requires.  At head_dim 256 the batch is at most 2,048, else
+    4,096.  ``scale`` (1e-30 to 1e30) defaults to ``head_dim ** -0.5``.  ``workspace`` (see new_attend_workspace) avoids
+    an allocation a call.
     """
     lib = _lib if _lib is not None else load_library()
     index, dtype, (num_pages, K, P, D), k_at, v_at, page_stride = _caches(k_cache, v_cache)
