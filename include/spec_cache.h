@@ -14,7 +14,10 @@
  *                      block tables and the slot map, all on the GPU;
  *   spec_cache_append  writes new keys and values to the mapped slots;
  *   spec_cache_attend  attention of the new tokens to a prefix that the whole
- *                      batch shares and to each sequence's own entries.
+ *                      batch shares and to each sequence's own entries;
+ *   spec_cache_append4, spec_cache_read4, spec_cache_attend4
+ *                      the same with a cache that is held in 4 bits, and its
+ *                      entries back in 16 (below).
  *
  * Layout.  All tensors are row-major and live in device memory.
  *   k_cache, v_cache  [num_pages, kv_heads, page_size, head_dim]  16-bit; the
@@ -49,6 +52,7 @@ extern "C" {
 /* Largest batch of one call. */
 #define SV_CACHE_MAX_BATCH 4096
 #define SV_CACHE_MAX_BATCH_D256 2048  /* spec_cache_attend at head_dim 256 (the batch's sums share the LDS) */
+#define SV_CACHE4_MAX_BATCH_D256 1024 /* spec_cache_attend4 there */
 
 /*
  * The tables of a batch.  num_pages is the number of pages of the caches;
@@ -182,6 +186,68 @@ sv_status_t spec_cache_attend(const sv_cache_attend_desc_t* desc, hipStream_t st
 /* Bytes of workspace that such a call needs, with or without a prefix; 0 for invalid sizes. */
 size_t spec_cache_attend_workspace_bytes(int32_t batch, int32_t max_new, int32_t q_heads, int32_t kv_heads,
                                          int32_t head_dim);
+
+/*
+ * Caches in 4 bits.  A value is held as an e2m1 number (0, 0.5, 1, 1.5, 2, 3, 4, 6
+ * and their negatives: codes 0 to 7, and 8 to 15), and each block of 32 values of a
+ * token and head (head_dim's last block may be shorter) shares a power of two,
+ * whose exponent + 127 is a byte: 4.25 bits a value.  This is the block format of
+ * the OCP microscaling specification (MXFP4), so the byte 255 makes its block NaN.
+ *   k_cache, v_cache  [num_pages, kv_heads, page_size * row] bytes, with
+ *                     row = head_dim / 2 + (head_dim + 31) / 32.  Of each page and
+ *                     head first the codes [page_size, head_dim / 2], an even
+ *                     value's in the low half of its byte, then the scales
+ *                     [page_size, (head_dim + 31) / 32].  Pages lie page_stride
+ *                     BYTES apart, a multiple of 16.
+ * The tables, slots and plans are the same as those of caches in 16 bits.
+ */
+
+/*
+ * spec_cache_append to such caches: each token's values are quantised as they
+ * are written, by themselves, so nothing that was written before changes.  A
+ * block's scale is the power of two that brings its largest magnitude into
+ * 3.5 .. 7, but not below 2^-23 (fp16) or 2^-125 (bf16), so that what is held are
+ * numbers of the storage type.  Values go to the nearest number that the codes have,
+ * those in the middle of two to the even code, those beyond 6 to 6: they move by
+ * at most a sixth of the block's largest magnitude.  A block with an infinity or NaN
+ * reads as NaN.
+ */
+sv_status_t spec_cache_append4(const sv_cache_append_desc_t* desc, hipStream_t stream);
+
+/*
+ * Entries of such caches, in 16 bits: k and v [batch, max_new, kv_heads, head_dim]
+ * of the tokens whose slots are named (they may be named more than once); rows
+ * whose slot is outside 0 .. num_pages * page_size - 1 (-1 among them) are not
+ * written.  What spec_cache_append4 wrote from the same type is returned exactly
+ * as it is held.  Strides and alignment are those of spec_cache_append, and rows
+ * do not lie on one another.
+ */
+typedef struct sv_cache_read_desc {
+    void* k;
+    void* v;
+    int64_t k_stride[3], v_stride[3];
+    const void* k_cache;
+    const void* v_cache;
+    int64_t page_stride;  /* bytes */
+    const int32_t* slots;
+    sv_dtype_t dtype;     /* SV_F16 or SV_BF16 */
+    int32_t batch, max_new, kv_heads, head_dim, num_pages, page_size;
+} sv_cache_read_desc_t;
+
+sv_status_t spec_cache_read4(const sv_cache_read_desc_t* desc, hipStream_t stream);
+
+/*
+ * spec_cache_attend over such caches: the same attention, of the values that
+ * spec_cache_read4 gives for `dtype`, with the same accuracy, limits and errors, but for at
+ * most SV_CACHE4_MAX_BATCH_D256 sequences at head_dim 256.  (Values
+ * that do not fit fp16, as bf16 may have written them, are infinite or lose
+ * bits there.)
+ */
+sv_status_t spec_cache_attend4(const sv_cache_attend_desc_t* desc, hipStream_t stream);
+
+/* Bytes of workspace that such a call needs, with or without a prefix; 0 for invalid sizes. */
+size_t spec_cache_attend4_workspace_bytes(int32_t batch, int32_t max_new, int32_t q_heads, int32_t kv_heads,
+                                          int32_t head_dim);
 
 #ifdef __cplusplus
 }

@@ -23,7 +23,8 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB_NAME = "libspec_verify.so"
 LIB_PATH = os.path.join(PKG_DIR, LIB_NAME)
 KERNEL_SOURCE = os.path.join(CSRC, "spec_verify.hip")
-CACHE_SOURCES = [os.path.join(CSRC, name) for name in ("cache.hip", "cache_attend.hip", "cache_attend_f16.hip")]
+CACHE_SOURCES = [os.path.join(CSRC, name) for name in ("cache.hip", "cache_attend.hip", "cache_attend_f16.hip", "cache4.hip",
+                                                        "cache4_attend.hip", "cache4_attend_f16.hip")]
 KERNEL_SOURCES = [KERNEL_SOURCE, *CACHE_SOURCES]
 HOST_SOURCES = [os.path.join(CSRC, "decode_loop.hip")]
 SOURCES = [*KERNEL_SOURCES, *HOST_SOURCES]

@@ -28,35 +28,12 @@
 
 #include <type_traits>
 
+#include "cache4.hpp"
+#include "cache_attend_args.hpp"
 #include "cache_split.hpp"
 #include "spec_cache.h"
 
 namespace sv {
-
-struct AttendArgs {
-    const uint16_t* q;
-    uint16_t* out;
-    int64_t q_stride[3], out_stride[3];
-    const uint16_t* k_cache;
-    const uint16_t* v_cache;
-    int64_t page_stride;
-    const int32_t* block_table;
-    const int32_t* prefix_table;
-    int32_t prefix_len, num_pages, q_heads;
-    float scale_log2, lazy;  // scale * log2(e); the rise of a maximum, in scores, that is let pass
-    Split split;
-    // workspace
-    int32_t* cum_tokens;  // [batch + 1] tokens before each sequence
-    uint32_t* cum_cost;   // [batch + 1] cost of the own tasks before each sequence's
-    float* part_out;      // parts: rows x head_dim, fp32
-    Totals* totals;       // of the split
-    float* part_max;      // maximum (scores as they come from the product)
-    float* part_sum;
-};
-
-// The kernels of each storage type are compiled by themselves.
-sv_status_t attend_f16(const AttendArgs& a, int32_t head_dim, hipStream_t stream);
-sv_status_t attend_bf16(const AttendArgs& a, int32_t head_dim, hipStream_t stream);
 
 namespace {
 
@@ -85,6 +62,13 @@ struct AttF16 {
     static __device__ __forceinline__ float value(uint32_t bits) {
         return (float)__builtin_bit_cast(_Float16, (uint16_t)bits);
     }
+    // 8 values that 4 bits each hold, and a scale (whose exponent counts): exact where they fit the type
+    static __device__ __forceinline__ u32x4 wide(uint32_t codes, float scale) {
+        return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, 0)),
+                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, 1)),
+                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, 2)),
+                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, 3))};
+    }
 };
 struct AttBF16 {
     // bf16 holds numbers up to fp32's largest, 2^128: so the sums of 2^20 largest weights (2^8 more
@@ -98,6 +82,20 @@ struct AttBF16 {
     }
     static __device__ __forceinline__ bool special(uint32_t bits) { return (bits & 0x7f80u) == 0x7f80u; }
     static __device__ __forceinline__ float value(uint32_t bits) { return __uint_as_float(bits << 16); }
+    static __device__ __forceinline__ u32x4 wide(uint32_t codes, float scale) {
+        return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0)),
+                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1)),
+                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2)),
+                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3))};
+    }
+};
+
+// How the caches hold their values: 16 bits each, or 4 (cache4.hpp).
+struct In16 {
+    static constexpr bool kFour = false;
+};
+struct In4 {
+    static constexpr bool kFour = true;
 };
 
 constexpr int kThreads = 256;
@@ -307,6 +305,20 @@ __device__ __forceinline__ void stage_barrier() {
     asm volatile("" : : : "memory");
 }
 
+// Own loads to LDS have landed, for this wave's own use.
+__device__ __forceinline__ void own_loads_landed() {
+    asm volatile("" : : : "memory");
+    __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0)
+    asm volatile("" : : : "memory");
+}
+
+// Own LDS reads are done, so that loads may come to where they read.
+__device__ __forceinline__ void lds_reads_done() {
+    asm volatile("" : : : "memory");
+    __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
+    asm volatile("" : : : "memory");
+}
+
 // Nothing is moved across: the reads written before a block of matrix products are
 // issued before it, so that their latency passes behind it.
 __device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }
@@ -344,11 +356,23 @@ __device__ __forceinline__ bool special_chunks(char* tile, bool clear) {
     return found != 0;
 }
 
+// A wave's 16 rows of a unit of K (V) in 4 bits, as they come from memory: codes, scales.
+template <int D>
+struct Raw {
+    static constexpr int kHalves = D / 16;              // half blocks of a row: 16 values, 8 bytes
+    static constexpr int kCodes = 16 * (D / 2);
+    static constexpr int kBytes = 16 * packed_row(D);   // of the run
+    static constexpr int kTotal = 4 * 2 * kBytes;       // K and V of the four waves
+};
+template <class C, int D>
+constexpr int kTiles = 2 * Shape<D>::kStage + (C::kFour ? Raw<D>::kTotal : 0);  // bytes of LDS
+
 // A workgroup's way through its run of the work: the segment at hand, and the
 // pages that this wave stages of it, a run of 16 rows of each unit.
-template <int D, Kind kKind>
+template <class C, int D, Kind kKind>
 struct Work {
     using S = Shape<D>;
+    using R = Raw<D>;
     const AttendArgs& a;
     const Totals& t;
     const Batch& batch;
@@ -360,6 +384,7 @@ struct Work {
     uint32_t at;                // place in the cost behind it
     uint32_t paged;             // lane l has the place in the caches of this wave's rows of unit `paged` + l
     uint32_t row_low, row_high;
+    uint32_t row_scales;        // in 4 bits: and how far behind it the scales of those rows are, in bytes
     bool poison;                // (one of them would have been on a page that there is not)
 
     // To the next segment; false if there is none.
@@ -412,8 +437,16 @@ struct Work {
             page = 0;
             poison = true;
         }
-        const int64_t row = (int64_t)page * a.page_stride + (int64_t)(g.kv_head << a.split.page_shift) * D +
-                            (first & ((1 << a.split.page_shift) - 1)) * D;
+        int64_t row;
+        if constexpr (C::kFour) {
+            const int in_page = first & ((1 << a.split.page_shift) - 1);
+            row = (int64_t)page * a.page_stride +
+                  (int64_t)(g.kv_head << a.split.page_shift) * packed_row(D) + in_page * (D / 2);
+            row_scales = (uint32_t)(((D / 2) << a.split.page_shift) - in_page * (D / 2 - packed_blocks(D)));
+        } else {
+            row = (int64_t)page * a.page_stride + (int64_t)(g.kv_head << a.split.page_shift) * D +
+                  (first & ((1 << a.split.page_shift) - 1)) * D;
+        }
         row_low = (uint32_t)row;
         row_high = (uint32_t)(row >> 32);
     }
@@ -426,6 +459,10 @@ struct Work {
         const uint32_t low = (uint32_t)__builtin_amdgcn_readlane((int)row_low, (int)(u - paged));
         const uint32_t high = (uint32_t)__builtin_amdgcn_readlane((int)row_high, (int)(u - paged));
         return (int64_t)((uint64_t)high << 32 | low);
+    }
+    // (of the unit that row_of was called for last)
+    __device__ __forceinline__ uint32_t scales_of(uint32_t u) const {
+        return (uint32_t)__builtin_amdgcn_readlane((int)row_scales, (int)(u - paged));
     }
     // And the last of its 16 rows that there is: those behind repeat it.
     __device__ __forceinline__ int last_row(uint32_t u) const {
@@ -448,11 +485,68 @@ struct Work {
                             cache + row + (kFull ? j * S::kRowsLoad * D : 0), offset);
         }
     }
+    // The same in 4 bits, in two steps: the rows as they are to a place of this wave's in LDS, and from there, widened to
+    // the storage type, to the tile.  (Between memory and the tile in registers they would take ones that there are not.)
+    __device__ __forceinline__ char* raw_of(char* smem, int v) const {
+        return smem + 2 * S::kStage + (uniform((int32_t)(threadIdx.x >> 6)) * 2 + v) * R::kBytes;
+    }
+    __device__ __forceinline__ void stage_raw(const uint16_t* cache, int64_t row, uint32_t scales, int v) const {
+        const uint32_t lane = (uint32_t)forget((int)threadIdx.x) & 63;
+        const uint32_t to = lds + 2 * S::kStage + (uniform((int32_t)(threadIdx.x >> 6)) * 2 + v) * R::kBytes;
+        const char* const from = (const char*)cache + row;
+#pragma unroll
+        for (int at = 0; at < R::kCodes; at += 1024)
+            if (R::kCodes - at >= 1024 || lane * 16 < (uint32_t)(R::kCodes - at)) load_to_lds(to + at, from + at, lane * 16);
+        if (lane * 16 < (uint32_t)(R::kBytes - R::kCodes)) load_to_lds(to + R::kCodes, from + scales, lane * 16);
+    }
+    // (Of the rows behind the last that there is, each repeats it.)
+    template <class T, bool kFull>
+    __device__ __forceinline__ void widen(char* smem, int v, int last, char* tile) const {
+        const int lane = forget((int)threadIdx.x) & 63;
+        const char* const raw = raw_of(smem, v);
+        char* const to = tile + uniform((int32_t)(threadIdx.x >> 6)) * (16 * S::kPitch * 2);
+        constexpr int kLoads = (16 * R::kHalves + 63) / 64;
+        u32x2 codes[kLoads];
+        uint32_t scale[kLoads];
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) {
+            const int at = lane + 64 * j;
+            if (16 * R::kHalves % 64 != 0 && at >= 16 * R::kHalves) continue;
+            const int of = at / R::kHalves, half = at % R::kHalves, r = kFull ? of : min(of, last);
+            codes[j] = *(const u32x2*)(raw + r * (D / 2) + half * 8);
+            scale[j] = *(const uint8_t*)(raw + R::kCodes + r * packed_blocks(D) + half / 2);
+        }
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) {
+            const int at = lane + 64 * j;
+            if (16 * R::kHalves % 64 != 0 && at >= 16 * R::kHalves) continue;
+            const int r = at / R::kHalves, half = at % R::kHalves;
+            const float by = __uint_as_float(scale[j] << 23);
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                *(u32x4*)(to + r * (S::kPitch * 2) + (((2 * half + i) ^ swizzle<D>(r)) * 16)) = T::wide(codes[j][i], by);
+        }
+    }
     __device__ __forceinline__ void stage_first() {
         const int64_t row = row_of(g.first);
         const int last = last_row(g.first);
-        stage<false>(a.k_cache, row, last, 0);
-        stage<false>(a.v_cache, row, last, S::kTile);
+        if constexpr (C::kFour) {
+            const uint32_t scales = scales_of(g.first);
+            stage_raw(a.k_cache, row, scales, 0);
+            stage_raw(a.v_cache, row, scales, 1);
+        } else {
+            stage<false>(a.k_cache, row, last, 0);
+            stage<false>(a.v_cache, row, last, S::kTile);
+        }
+    }
+    template <class T>
+    __device__ __forceinline__ void widen_first(char* smem) const {
+        if constexpr (C::kFour) {
+            const int last = last_row(g.first);
+            own_loads_landed();
+            widen<T, false>(smem, 0, last, smem);
+            widen<T, false>(smem, 1, last, smem + S::kTile);
+        }
     }
 };
 
@@ -474,8 +568,8 @@ struct Work {
 // vector units, the matrix units make the next one's scores, product by product in
 // between (the two overlap in one wave only if its instructions alternate).  Both
 // are staged two deep in LDS, with one barrier between units.
-template <class T, int D, int WR, Kind kKind>
-__device__ __forceinline__ bool segment(Work<D, kKind>& work, char* smem, float (*wave_stats)[2][32], int* poison_flag,
+template <class T, class C, int D, int WR, Kind kKind>
+__device__ __forceinline__ bool segment(Work<C, D, kKind>& work, char* smem, float (*wave_stats)[2][32], int* poison_flag,
                                         int* special_flag) {
     using S = Shape<D>;
     using V8 = typename T::V8;
@@ -598,6 +692,7 @@ __device__ __forceinline__ bool segment(Work<D, kKind>& work, char* smem, float 
     // even units lie in the first two tiles of LDS (K, V), its odd ones in the others.  `full`: it and the two units
     // behind it are of the same segment, of one table, and every row sees all their keys.
     int64_t row = 0;  // this wave's first row of the unit whose K was staged last
+    uint32_t scales = 0;
     auto step = [&](auto full, uint32_t u, auto odd, f32x16(&p)[NS], f32x16(&next)[NS]) {
         constexpr bool kFull = decltype(full)::value;
         constexpr int kHere = decltype(odd)::value * S::kStage, kThere = S::kStage - kHere;
@@ -616,10 +711,28 @@ __device__ __forceinline__ bool segment(Work<D, kKind>& work, char* smem, float 
         stage_barrier();  // K of the next unit and V of this one are there, and every wave has done with those before
         if (more) {
             shift = forget(shift);  // (else the weights' arguments are made before this branch, for both)
-            work.template stage<kFull>(a.v_cache, row, kFull ? 0 : work.last_row(u + 1), kThere + S::kTile);
-            if (kFull || u + 2 < g.end) {
-                row = work.row_of(u + 2);
-                work.template stage<kFull>(a.k_cache, row, kFull ? 0 : work.last_row(u + 2), kHere);
+            if constexpr (C::kFour) {
+                // (what is on its way comes a unit earlier: it has to be widened before the barrier)
+                work.template widen<T, kFull>(smem, 1, kFull ? 0 : work.last_row(u + 1), smem + kThere + S::kTile);
+                if (kFull || u + 2 < g.end) {
+                    in_order();
+                    work.template widen<T, kFull>(smem, 0, kFull ? 0 : work.last_row(u + 2), smem + kHere);
+                    lds_reads_done();
+                    in_order();
+                    work.stage_raw(a.v_cache, row, scales, 1);
+                    if (u + 3 < g.end) {
+                        row = work.row_of(u + 3);
+                        scales = work.scales_of(u + 3);
+                        work.stage_raw(a.k_cache, row, scales, 0);
+                    }
+                }
+                in_order();
+            } else {
+                work.template stage<kFull>(a.v_cache, row, kFull ? 0 : work.last_row(u + 1), kThere + S::kTile);
+                if (kFull || u + 2 < g.end) {
+                    row = work.row_of(u + 2);
+                    work.template stage<kFull>(a.k_cache, row, kFull ? 0 : work.last_row(u + 2), kHere);
+                }
             }
             const char* const tile = smem + kThere;
             V8 k[kAhead + 1];
@@ -709,7 +822,13 @@ __device__ __forceinline__ bool segment(Work<D, kKind>& work, char* smem, float 
         stage_barrier();  // the first unit
         if (g.first + 1 < g.end) {
             row = work.row_of(g.first + 1);
-            work.template stage<false>(a.k_cache, row, work.last_row(g.first + 1), S::kStage);
+            if constexpr (C::kFour) {
+                scales = work.scales_of(g.first + 1);
+                work.stage_raw(a.k_cache, row, scales, 0);
+                work.stage_raw(a.v_cache, row, scales, 1);
+            } else {
+                work.template stage<false>(a.k_cache, row, work.last_row(g.first + 1), S::kStage);
+            }
         }
         float most = -INFINITY;
 #pragma unroll
@@ -724,6 +843,19 @@ __device__ __forceinline__ bool segment(Work<D, kKind>& work, char* smem, float 
             scores[0][m % NS] = T::mma(k[m % (kAhead + 1)], q[m / NS], scores[0][m % NS]);
         }
         in_order();
+        if constexpr (C::kFour) {
+            if (g.first + 1 < g.end) {
+                const int last = work.last_row(g.first + 1);
+                own_loads_landed();
+                work.template widen<T, false>(smem, 0, last, smem + S::kStage);
+            }
+            if (g.first + 2 < g.end) {
+                lds_reads_done();
+                row = work.row_of(g.first + 2);
+                scales = work.scales_of(g.first + 2);
+                work.stage_raw(a.k_cache, row, scales, 0);
+            }
+        }
 #pragma unroll
         for (int s = 0; s < NS; ++s)
 #pragma unroll
@@ -840,19 +972,23 @@ __device__ __forceinline__ bool segment(Work<D, kKind>& work, char* smem, float 
     lds_barrier();  // every wave has done with the tiles
     if (more) work.stage_first();  // (into the first two; what follows works in the others)
     finish(forget(lane), whole, place);
+    if (more) work.template widen_first<T>(smem);
     lds_barrier();  // they and the flag are free again
     if (tid == 0) *poison_flag = 0;
     return more;
 }
 
-template <class T, int D, int WR, Kind kKind>
+template <class T, class C, int D, int WR, Kind kKind>
 __device__ __forceinline__ void run(const AttendArgs& a, const Totals& t, const Deal& deal, const Batch& batch, uint32_t w,
                                     char* smem, float (*wave_stats)[2][32], int* poison_flag, int* special_flag) {
-    Work<D, kKind> work{a, t, batch, (uint32_t)(uintptr_t)(SV_LDS char*)smem, w, group_start(deal, w + 1),
-                        {}, 0, false, group_start(deal, w), 0, 0, 0, false};
+    Work<C, D, kKind> work{a, t, batch, (uint32_t)(uintptr_t)(SV_LDS char*)smem, w, group_start(deal, w + 1),
+                           {}, 0, false, group_start(deal, w), 0, 0, 0, 0, false};
     bool more = work.advance();
-    if (more) work.stage_first();
-    while (more) more = segment<T, D, WR>(work, smem, wave_stats, poison_flag, special_flag);
+    if (more) {
+        work.stage_first();
+        work.template widen_first<T>(smem);
+    }
+    while (more) more = segment<T, C, D, WR>(work, smem, wave_stats, poison_flag, special_flag);
 }
 
 // Workgroups go round the 8 XCDs.  Those of one XCD take adjoining runs of the tasks
@@ -864,14 +1000,14 @@ __device__ __forceinline__ uint32_t place_in_xcd(uint32_t block, uint32_t groups
 
 // kPrefix and kRows: waves that split the rows of the prefix's tasks (0: there are
 // none, a sequence's tasks begin with it) and of the sequences' own.
-template <class T, int D, int kPrefix, int kRows>
+template <class T, class C, int D, int kPrefix, int kRows>
 __global__ void __launch_bounds__(kThreads, (D > 128 ? 1 : 2)) attend_kernel(AttendArgs a) {
     extern __shared__ __attribute__((aligned(16))) char smem[];
     __shared__ uint32_t wave_sums[4][2];
     __shared__ float wave_stats[4][2][32];
     __shared__ int poison_flag, special_flag;
     const Split& split = a.split;
-    int32_t* const words = (int32_t*)(smem + 2 * Shape<D>::kStage);
+    int32_t* const words = (int32_t*)(smem + kTiles<C, D>);
     const Batch batch{words, (uint32_t*)words + split.batch + 1, words + 2 * (split.batch + 1)};
     if (threadIdx.x == 0) poison_flag = special_flag = 0;
     const Totals t = sum_batch(split, batch, wave_sums);
@@ -883,13 +1019,13 @@ __global__ void __launch_bounds__(kThreads, (D > 128 ? 1 : 2)) attend_kernel(Att
         }
     if constexpr (kPrefix == 0) {
         if (blockIdx.x < t.own.groups)
-            run<T, D, kRows, kJoined>(a, t, t.own, batch, place_in_xcd(blockIdx.x, t.own.groups), smem, wave_stats,
+            run<T, C, D, kRows, kJoined>(a, t, t.own, batch, place_in_xcd(blockIdx.x, t.own.groups), smem, wave_stats,
                                       &poison_flag, &special_flag);
     } else if (blockIdx.x < t.prefix.groups) {
-        run<T, D, kPrefix, kShared>(a, t, t.prefix, batch, place_in_xcd(blockIdx.x, t.prefix.groups), smem, wave_stats,
+        run<T, C, D, kPrefix, kShared>(a, t, t.prefix, batch, place_in_xcd(blockIdx.x, t.prefix.groups), smem, wave_stats,
                                     &poison_flag, &special_flag);
     } else if (blockIdx.x - t.prefix.groups < t.own.groups) {
-        run<T, D, kRows, kOwn>(a, t, t.own, batch, blockIdx.x - t.prefix.groups, smem, wave_stats, &poison_flag,
+        run<T, C, D, kRows, kOwn>(a, t, t.own, batch, blockIdx.x - t.prefix.groups, smem, wave_stats, &poison_flag,
                                &special_flag);
     }
 }
@@ -1162,12 +1298,12 @@ __global__ void __launch_bounds__(kThreads) attend_join_tasks_kernel(AttendArgs 
 template <int D>
 constexpr int kMaxTaskRows = D > 128 ? 64 : 128;
 
-template <class T, int D>
+template <class T, class C, int D>
 sv_status_t launch(const AttendArgs& a, hipStream_t stream) {
-    const size_t lds = 2 * Shape<D>::kStage + 3 * sizeof(int32_t) * ((size_t)a.split.batch + 1);
+    const size_t lds = kTiles<C, D> + 3 * sizeof(int32_t) * ((size_t)a.split.batch + 1);
     const uint32_t groups = (uint32_t)a.split.plan.groups;
     auto go = [&](auto prefix, auto own) {
-        hipLaunchKernelGGL((attend_kernel<T, D, decltype(prefix)::value, decltype(own)::value>), dim3(groups),
+        hipLaunchKernelGGL((attend_kernel<T, C, D, decltype(prefix)::value, decltype(own)::value>), dim3(groups),
                            dim3(kThreads), lds, stream, a);
     };
     constexpr std::integral_constant<int, 0> k0{};
@@ -1202,14 +1338,14 @@ sv_status_t launch(const AttendArgs& a, hipStream_t stream) {
     return hipGetLastError() == hipSuccess ? SV_OK : SV_ERR_HIP;
 }
 
-template <class T>
+template <class T, class C>
 sv_status_t launch_dim(const AttendArgs& a, int32_t head_dim, hipStream_t stream) {
     switch (head_dim) {
-        case 64: return launch<T, 64>(a, stream);
-        case 80: return launch<T, 80>(a, stream);
-        case 96: return launch<T, 96>(a, stream);
-        case 128: return launch<T, 128>(a, stream);
-        default: return launch<T, 256>(a, stream);
+        case 64: return launch<T, C, 64>(a, stream);
+        case 80: return launch<T, C, 80>(a, stream);
+        case 96: return launch<T, C, 96>(a, stream);
+        case 128: return launch<T, C, 128>(a, stream);
+        default: return launch<T, C, 256>(a, stream);
     }
 }
 

@@ -8,6 +8,7 @@
 
 #include <initializer_list>
 
+#include "cache4.hpp"
 #include "spec_cache.h"
 
 namespace sv {
@@ -54,6 +55,15 @@ inline sv_status_t check_cache(sv_dtype_t dtype, int32_t batch, int32_t max_new,
         !page_size_ok(page_size) || (int64_t)num_pages * page_size > INT_MAX)
         return SV_ERR_SHAPE;
     if (page_stride < (int64_t)kv_heads * page_size * head_dim || page_stride % 8 != 0) return SV_ERR_PARAM;
+    return SV_OK;
+}
+
+// The same of caches in 4 bits, whose strides are in bytes.
+inline sv_status_t check_cache4(sv_dtype_t dtype, int32_t batch, int32_t max_new, int32_t kv_heads, int32_t head_dim,
+                                int32_t num_pages, int32_t page_size, int64_t page_stride) {
+    const sv_status_t st = check_cache(dtype, batch, max_new, kv_heads, head_dim, num_pages, page_size, INT64_MAX - 7);
+    if (st != SV_OK) return st;
+    if (page_stride < (int64_t)kv_heads * page_size * packed_row(head_dim) || page_stride % 16 != 0) return SV_ERR_PARAM;
     return SV_OK;
 }
 
@@ -162,12 +172,20 @@ inline size_t attend_workspace_bytes(int32_t batch, int32_t max_new, int32_t q_h
     return (most + 255) / 256 * 256;
 }
 
-inline sv_status_t check_attend(const sv_cache_attend_desc_t& d) {
+// Caches in 4 bits: at head_dim 256 a unit's bytes as they come from memory share the LDS, too.
+inline size_t attend4_workspace_bytes(int32_t batch, int32_t max_new, int32_t q_heads, int32_t kv_heads,
+                                      int32_t head_dim) {
+    if (head_dim > 128 && batch > SV_CACHE4_MAX_BATCH_D256) return 0;
+    return attend_workspace_bytes(batch, max_new, q_heads, kv_heads, head_dim);
+}
+
+template <class CheckCache = decltype(&check_cache)>
+inline sv_status_t check_attend(const sv_cache_attend_desc_t& d, CheckCache check = check_cache) {
     if (d.q == nullptr || d.out == nullptr || d.k_cache == nullptr || d.v_cache == nullptr || d.block_table == nullptr ||
         d.lengths == nullptr || d.workspace == nullptr || (d.prefix_len != 0 && d.prefix_table == nullptr))
         return SV_ERR_NULL;
-    const sv_status_t st = check_cache(d.dtype, d.batch, d.max_new, d.kv_heads, d.head_dim, d.num_pages, d.page_size,
-                                       d.page_stride);
+    const sv_status_t st =
+        check(d.dtype, d.batch, d.max_new, d.kv_heads, d.head_dim, d.num_pages, d.page_size, d.page_stride);
     if (st != SV_OK) return st;
     if (!attend_sizes_ok(d.batch, d.max_new, d.q_heads, d.kv_heads, d.head_dim) || d.max_pages < 1 ||
         (int64_t)d.batch * d.max_pages > INT_MAX || (int64_t)d.max_pages * d.page_size > INT_MAX || d.prefix_len < 0 ||
@@ -185,6 +203,12 @@ inline sv_status_t check_attend(const sv_cache_attend_desc_t& d) {
         d.workspace_bytes < attend_workspace_bytes(d.batch, d.max_new, d.q_heads, d.kv_heads, d.head_dim))
         return SV_ERR_WORKSPACE;
     return SV_OK;
+}
+
+inline sv_status_t check_attend4(const sv_cache_attend_desc_t& d) {
+    const sv_status_t st = check_attend(d, check_cache4);
+    if (st != SV_OK) return st;
+    return d.head_dim > 128 && d.batch > SV_CACHE4_MAX_BATCH_D256 ? SV_ERR_SHAPE : SV_OK;
 }
 
 }  // namespace sv

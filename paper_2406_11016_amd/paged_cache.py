@@ -14,7 +14,10 @@ This module has the cache's operators, each a call of the HIP library
   mapped slots;
 * :func:`attend` (:meth:`PagedCache.attend`) is the attention of the new tokens
   to a prefix that the whole batch shares, whose reads the sequences' tokens
-  share, and to each sequence's own entries.
+  share, and to each sequence's own entries;
+* :func:`append4`, :func:`read4` and :func:`attend4` work on caches that are held
+  in 4 bits (4.25 with the scales), which the methods of :class:`PagedCache` do
+  with storage made with ``bits=4``.
 
 A step of a target model with such a cache::
 
@@ -49,6 +52,10 @@ SYMBOLS = (
     "spec_cache_append",
     "spec_cache_attend",
     "spec_cache_attend_workspace_bytes",
+    "spec_cache_append4",
+    "spec_cache_read4",
+    "spec_cache_attend4",
+    "spec_cache_attend4_workspace_bytes",
 )
 
 _i64x3 = ctypes.c_int64 * 3
@@ -66,6 +73,11 @@ class AppendDesc(ctypes.Structure):
                 ("v_cache", _vp), ("page_stride", ctypes.c_int64), ("slots", _vp), ("dtype", ctypes.c_int),
                 ("batch", _i32), ("max_new", _i32), ("kv_heads", _i32), ("head_dim", _i32), ("num_pages", _i32),
                 ("page_size", _i32)]
+
+
+class ReadDesc(ctypes.Structure):
+    """``sv_cache_read_desc_t``."""
+    _fields_ = AppendDesc._fields_
 
 
 class AttendDesc(ctypes.Structure):
@@ -96,10 +108,14 @@ def load_library() -> ctypes.CDLL:
     lib.spec_cache_plan.argtypes = [ctypes.POINTER(Tables), _vp, _vp, _vp, _i32, _i32, _vp, _vp, _vp]
     lib.spec_cache_append.argtypes = [_vp, _vp]
     lib.spec_cache_attend.argtypes = [_vp, _vp]
-    for f in (lib.spec_cache_init, lib.spec_cache_plan, lib.spec_cache_append, lib.spec_cache_attend):
+    for f in (lib.spec_cache_append4, lib.spec_cache_read4, lib.spec_cache_attend4):
+        f.argtypes = [_vp, _vp]
+    for f in (lib.spec_cache_init, lib.spec_cache_plan, lib.spec_cache_append, lib.spec_cache_attend, lib.spec_cache_append4,
+              lib.spec_cache_read4, lib.spec_cache_attend4):
         f.restype = ctypes.c_int
-    lib.spec_cache_attend_workspace_bytes.argtypes = [_i32] * 5
-    lib.spec_cache_attend_workspace_bytes.restype = _sz
+    for f in (lib.spec_cache_attend_workspace_bytes, lib.spec_cache_attend4_workspace_bytes):
+        f.argtypes = [_i32] * 5
+        f.restype = _sz
     _lib = lib
     return lib
 
@@ -205,10 +221,17 @@ def attend(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, block_
     """
     lib = _lib if _lib is not None else load_library()
     index, dtype, (num_pages, K, P, D), k_at, v_at, page_stride = _caches(k_cache, v_cache)
+    if q.dim() != 4 or q.shape[3] != D:
+        raise SpecVerifyError(f"q must be [batch, tokens, q_heads, {D}] for these caches; it is {list(q.shape)}")
+    return _attend(lib.spec_cache_attend, "spec_cache_attend", new_attend_workspace, q, index, dtype, num_pages, K, P, k_at,
+                   v_at, page_stride, block_table, lengths, counts, prefix_table, prefix_len, scale, out, workspace)
+
+
+def _attend(f, what, new_workspace, q, index, dtype, num_pages, K, P, k_at, v_at, page_stride, block_table, lengths, counts,
+            prefix_table, prefix_len, scale, out, workspace) -> torch.Tensor:
+    """attend() and attend4(), of which the caches are known to be what they should be."""
     shape = q.shape
-    if len(shape) != 4 or shape[3] != D:
-        raise SpecVerifyError(f"q must be [batch, tokens, q_heads, {D}] for these caches; it is {list(shape)}")
-    B, n, H, _ = shape
+    B, n, H, D = shape
     q_at, qb, qt, qh = _rows("q", q, shape, index, dtype)
     if block_table.dim() != 2:
         raise SpecVerifyError("block_table must be [batch, max_pages]")
@@ -226,16 +249,135 @@ def attend(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, block_
             torch.zeros(shape, dtype=dtype, device=q.device)
     out_at, ob, ot, oh = _rows("out", out, shape, index, dtype)
     if workspace is None:
-        workspace = new_attend_workspace(B, n, H, K, D, q.device)
+        workspace = new_workspace(B, n, H, K, D, q.device)
     elif not workspace.is_contiguous() or workspace.get_device() != index:
         raise SpecVerifyError(f"workspace must be a contiguous tensor on device {index}")
-    _call(index, lib.spec_cache_attend, "spec_cache_attend",
+    _call(index, f, what,
           _pack_attend(q_at, out_at, qb, qt, qh, ob, ot, oh, k_at, v_at, page_stride, block_table.data_ptr(),
                        lengths.data_ptr(), 0 if counts is None else counts.data_ptr(),
                        prefix_table.data_ptr() if prefix_len else 0, prefix_len, DTYPE_CODES[dtype], B, n, H, K, D, M,
                        num_pages, P, D ** -0.5 if scale is None else scale, workspace.data_ptr(),
                        workspace.numel() * workspace.element_size()))
     return out
+
+
+# ---------------------------------------------------------------------------
+# caches in 4 bits
+# ---------------------------------------------------------------------------
+
+def row_bytes4(head_dim: int) -> int:
+    """Bytes of a token and head in a cache of 4 bits: its codes and its scales."""
+    return head_dim // 2 + (head_dim + 31) // 32
+
+
+def _caches4(k_cache: torch.Tensor, v_cache: torch.Tensor, head_dim: int):
+    """A pair of caches in 4 bits: device, pages, heads, page size, addresses and the stride of their pages in bytes."""
+    index, shape, strides = k_cache.get_device(), k_cache.shape, k_cache.stride()
+    if index < 0 or len(shape) != 3 or k_cache.dtype != torch.uint8:
+        raise SpecVerifyError("caches in 4 bits must be uint8 device tensors [num_pages, kv_heads, bytes of a page]")
+    if v_cache.shape != shape or v_cache.dtype != torch.uint8 or v_cache.get_device() != index or \
+            v_cache.stride() != strides:
+        raise SpecVerifyError("k_cache and v_cache must be alike in shape, strides, dtype and device")
+    (n, h, size), (sn, sh, sb) = shape, strides
+    row = row_bytes4(head_dim)
+    if size % row:
+        raise SpecVerifyError(f"{size} bytes of a page and head are no whole number of tokens of {row} bytes "
+                              f"(head_dim {head_dim})")
+    if n == 1:
+        sn = max(sn, h * size)
+    k, v = k_cache.data_ptr(), v_cache.data_ptr()
+    if sb != 1 or (h > 1 and sh != size) or (sn | k | v) & 15:
+        raise SpecVerifyError("a cache's pages must be dense and aligned to 16 bytes")
+    return index, n, h, size // row, k, v, sn
+
+
+def _dtype4(what: str, dtype) -> int:
+    code = DTYPE_CODES.get(dtype)
+    if code is None:
+        raise SpecVerifyError(f"{what} must be float16 or bfloat16; got {dtype}")
+    return code
+
+
+def append4(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, slots: torch.Tensor) -> None:
+    """append() to caches in 4 bits (uint8; see PagedCache.new_storage): ``k`` and ``v [B, n, kv_heads, head_dim]`` are
+    quantised as they are written (spec_cache_append4)."""
+    lib = _lib if _lib is not None else load_library()
+    shape, dtype = k.shape, k.dtype
+    if len(shape) != 4:
+        raise SpecVerifyError(f"k and v must be [batch, tokens, kv_heads, head_dim]; k is {list(shape)}")
+    B, n, H, d = shape
+    code = _dtype4("k and v", dtype)
+    index, num_pages, h, p, k_at, v_at, page_stride = _caches4(k_cache, v_cache, d)
+    if H != h:
+        raise SpecVerifyError(f"k and v must have {h} heads for these caches; k is {list(shape)}")
+    k_from, kb, kt, kh = _rows("k", k, shape, index, dtype)
+    v_from, vb, vt, vh = _rows("v", v, shape, index, dtype)
+    _int32("slots", slots, (B, n), index)
+    _call(index, lib.spec_cache_append4, "spec_cache_append4",
+          _pack_append(k_from, v_from, kb, kt, kh, vb, vt, vh, k_at, v_at, page_stride, slots.data_ptr(), code, B, n, h, d,
+                       num_pages, p))
+
+
+def read4(k_cache: torch.Tensor, v_cache: torch.Tensor, slots: torch.Tensor, head_dim: Optional[int] = None, dtype=None, *,
+          out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Keys and values of the slots that ``slots`` (int32 ``[B, n]``) names, back from caches in 4 bits.
+
+    Returns ``(k, v)``, ``[B, n, kv_heads, head_dim]`` of ``dtype`` (float16 or bfloat16, what they were written from).
+    Rows whose slot is outside the cache (-1) are not written; new tensors are zero there.  ``out`` gives the tensors,
+    and head_dim and dtype with them; they do not overlap.
+    """
+    lib = _lib if _lib is not None else load_library()
+    if slots.dim() != 2:
+        raise SpecVerifyError("slots must be [batch, tokens]")
+    B, n = slots.shape
+    if out is None:
+        if head_dim is None or k_cache.dim() != 3:
+            raise SpecVerifyError("read4 needs head_dim and dtype, or out, and caches [num_pages, kv_heads, bytes of a page]")
+        _dtype4("dtype", dtype)
+        out = tuple(torch.zeros(B, n, k_cache.shape[1], head_dim, dtype=dtype, device=k_cache.device) for _ in range(2))
+    k, v = out
+    shape = k.shape
+    if len(shape) != 4 or (head_dim is not None and shape[3] != head_dim) or (dtype is not None and k.dtype != dtype):
+        raise SpecVerifyError(f"out must be two tensors [batch, tokens, kv_heads, head_dim]; the first is {k.dtype} "
+                              f"{list(shape)}")
+    d, code = shape[3], _dtype4("out", k.dtype)
+    index, num_pages, h, p, k_at, v_at, page_stride = _caches4(k_cache, v_cache, d)
+    k_to, kb, kt, kh = _rows("out[0]", k, (B, n, h, d), index, k.dtype)
+    v_to, vb, vt, vh = _rows("out[1]", v, (B, n, h, d), index, k.dtype)
+    _int32("slots", slots, (B, n), index)
+    _call(index, lib.spec_cache_read4, "spec_cache_read4",
+          _pack_append(k_to, v_to, kb, kt, kh, vb, vt, vh, k_at, v_at, page_stride, slots.data_ptr(), code, B, n, h, d,
+                       num_pages, p))
+    return k, v
+
+
+def attend4_workspace_bytes(batch: int, max_new: int, q_heads: int, kv_heads: int, head_dim: int) -> int:
+    n = load_library().spec_cache_attend4_workspace_bytes(batch, max_new, q_heads, kv_heads, head_dim)
+    if n == 0:
+        raise SpecVerifyError(f"invalid sizes: batch={batch} max_new={max_new} q_heads={q_heads} kv_heads={kv_heads} "
+                              f"head_dim={head_dim}")
+    return int(n)
+
+
+def new_attend4_workspace(batch: int, max_new: int, q_heads: int, kv_heads: int, head_dim: int, device) -> torch.Tensor:
+    """A workspace for attend4() at these sizes (reusable across ordered calls; needs no initialisation)."""
+    return torch.empty(attend4_workspace_bytes(batch, max_new, q_heads, kv_heads, head_dim), dtype=torch.uint8,
+                       device=device)
+
+
+def attend4(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, block_table: torch.Tensor,
+            lengths: torch.Tensor, counts: Optional[torch.Tensor] = None, *,
+            prefix_table: Optional[torch.Tensor] = None, prefix_len: int = 0, scale: Optional[float] = None,
+            out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """attend() over caches in 4 bits: of the values that read4() gives for q's type.  All else is as there, but that at
+    head_dim 256 the batch is at most 1,024; the ``workspace`` is new_attend4_workspace()'s."""
+    lib = _lib if _lib is not None else load_library()
+    if q.dim() != 4:
+        raise SpecVerifyError(f"q must be [batch, tokens, q_heads, head_dim]; it is {list(q.shape)}")
+    _dtype4("q", q.dtype)
+    index, num_pages, K, P, k_at, v_at, page_stride = _caches4(k_cache, v_cache, q.shape[3])
+    return _attend(lib.spec_cache_attend4, "spec_cache_attend4", new_attend4_workspace, q, index, q.dtype, num_pages, K, P,
+                   k_at, v_at, page_stride, block_table, lengths, counts, prefix_table, prefix_len, scale, out, workspace)
 
 
 class PagedCache:
@@ -339,11 +481,18 @@ class PagedCache:
             raise SpecVerifyError(f"a prefix of {length} tokens does not fit {self.prefix_table.numel()} pages")
         self.prefix_len = length
 
-    def new_storage(self, kv_heads: int, head_dim: int, dtype) -> Tuple[torch.Tensor, torch.Tensor]:
-        """Key and value caches of one layer, ``[num_pages, kv_heads, page_size, head_dim]`` (uninitialised)."""
+    def new_storage(self, kv_heads: int, head_dim: int, dtype, *, bits: int = 16) -> Tuple[torch.Tensor, torch.Tensor]:
+        """Key and value caches of one layer, ``[num_pages, kv_heads, page_size, head_dim]`` (uninitialised).  With
+        ``bits=4`` what is appended is quantised to 4 bits: uint8 ``[num_pages, kv_heads, bytes of a page]``, a little
+        more than a quarter of the memory."""
         if dtype not in DTYPE_CODES:
             raise SpecVerifyError(f"caches hold one of {list(DTYPE_CODES)}; got {dtype}")
+        if bits not in (4, 16) or (bits == 4 and head_dim % 8):
+            raise SpecVerifyError(f"caches hold their values in 16 or (head_dim a multiple of 8) 4 bits; got bits={bits}, "
+                                  f"head_dim={head_dim}")
         shape = (self.num_pages, kv_heads, self.page_size, head_dim)
+        if bits == 4:
+            shape, dtype = (self.num_pages, kv_heads, self.page_size * row_bytes4(head_dim)), torch.uint8
         return tuple(torch.empty(shape, dtype=dtype, device=self.device) for _ in range(2))
 
     def plan(self, n: int, *, new_tokens: Optional[torch.Tensor] = None, accepted_len: Optional[torch.Tensor] = None,
@@ -369,31 +518,50 @@ class PagedCache:
         self.slots, self.positions = slots, positions
         return slots, positions
 
-    def _described(self, k_cache: torch.Tensor) -> None:
-        """Slots and block tables count in the tables' pages: a cache has such pages, and as many or more."""
-        if k_cache.dim() != 4 or k_cache.shape[2] != self.page_size or k_cache.shape[0] < self.num_pages:
+    def _described(self, k_cache: torch.Tensor, head_dim: int) -> bool:
+        """Slots and block tables count in the tables' pages: a cache has such pages, and as many or more.  Whether it
+        is one in 4 bits."""
+        four = k_cache.dtype == torch.uint8
+        page = (3, self.page_size * row_bytes4(head_dim)) if four else (4, self.page_size)
+        if (k_cache.dim(), *k_cache.shape[2:3]) != page or k_cache.shape[0] < self.num_pages:
             raise SpecVerifyError(f"the tables are of {self.num_pages} pages of {self.page_size} tokens; the cache is "
                                   f"{list(k_cache.shape)}")
+        return four
 
     def append(self, k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor) -> None:
         """The planned tokens' keys and values ``[B, n, kv_heads, head_dim]`` into their slots."""
-        self._described(k_cache)
-        append(k, v, k_cache, v_cache, self.slots)
+        (append4 if self._described(k_cache, k.shape[-1]) else append)(k, v, k_cache, v_cache, self.slots)
 
     def append_prefix(self, k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
                       start: int = 0) -> None:
         """Keys and values ``[1, n, kv_heads, head_dim]`` of the prefix's tokens from ``start`` on."""
-        self._described(k_cache)
+        write = append4 if self._described(k_cache, k.shape[-1]) else append
         end = start + k.shape[1]
         if start < 0 or end > self.prefix_table.numel() * self.page_size:
             raise SpecVerifyError(f"prefix tokens {start} to {end} do not fit {self.prefix_table.numel()} pages")
         pages = self.prefix_table[torch.arange(start, end, device=self.device) // self.page_size]
         at = torch.arange(start, end, device=self.device, dtype=torch.int32) % self.page_size
-        append(k, v, k_cache, v_cache, (pages * self.page_size + at)[None])
+        write(k, v, k_cache, v_cache, (pages * self.page_size + at)[None])
 
-    def _workspace(self, *sizes: int) -> torch.Tensor:
+    def read(self, k_cache: torch.Tensor, v_cache: torch.Tensor, head_dim: int, dtype, *, start: int = 0,
+             n: Optional[int] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+        """Keys and values of every sequence's own tokens ``start`` to ``start + n - 1`` (up to the last place of the
+        tables without ``n``), back from caches in 4 bits: ``(k, v)``, ``[B, n, kv_heads, head_dim]`` of ``dtype``, zero
+        behind a sequence's last planned token."""
+        if k_cache.dtype != torch.uint8 or not self._described(k_cache, head_dim):
+            raise SpecVerifyError("read() is for caches in 4 bits")
+        end = self.max_pages * self.page_size if n is None else start + n
+        if not 0 <= start < end <= self.max_pages * self.page_size:
+            raise SpecVerifyError(f"tokens {start} to {end} are not within the tables' {self.max_pages} pages a sequence")
+        at = torch.arange(start, end, device=self.device, dtype=torch.int32)
+        pages = self.block_table[:, at // self.page_size]
+        there = (at < (self.lengths + self.counts.clamp(min=0))[:, None]) & (pages >= 0)
+        slots = torch.where(there, pages * self.page_size + at % self.page_size, -1)
+        return read4(k_cache, v_cache, slots, head_dim, dtype)
+
+    def _workspace(self, four: bool, *sizes: int) -> torch.Tensor:
         """One for each power of two of bytes, and none is given up: captured graphs may hold it."""
-        size = 1 << (attend_workspace_bytes(*sizes) - 1).bit_length()
+        size = 1 << ((attend4_workspace_bytes if four else attend_workspace_bytes)(*sizes) - 1).bit_length()
         if size not in self._workspaces:
             self._workspaces[size] = torch.empty(size, dtype=torch.uint8, device=self.device)
         return self._workspaces[size]
@@ -404,10 +572,11 @@ class PagedCache:
         and shared by all layers: calls have to be ordered."""
         if q.dim() != 4:
             raise SpecVerifyError(f"q must be [batch, tokens, q_heads, head_dim]; it is {list(q.shape)}")
-        self._described(k_cache)
-        key = (q.shape, k_cache.shape[1])
+        four = self._described(k_cache, q.shape[3])
+        key = (q.shape, k_cache.shape[1], four)
         workspace = self._workspace_of.get(key)
         if workspace is None:
-            workspace = self._workspace_of[key] = self._workspace(*q.shape[:3], k_cache.shape[1], q.shape[3])
-        return attend(q, k_cache, v_cache, self.block_table, self.lengths, self.counts, prefix_table=self.prefix_table,
-                      prefix_len=self.prefix_len, scale=scale, out=out, workspace=workspace)
+            workspace = self._workspace_of[key] = self._workspace(four, *q.shape[:3], k_cache.shape[1], q.shape[3])
+        return (attend4 if four else attend)(q, k_cache, v_cache, self.block_table, self.lengths, self.counts,
+                                             prefix_table=self.prefix_table, prefix_len=self.prefix_len, scale=scale,
+                                             out=out, workspace=workspace)
