@@ -6,7 +6,7 @@
 namespace sv {
 
 sv_status_t attend_bf16(const AttendArgs& a, int32_t head_dim, hipStream_t stream) {
-    return launch_dim<AttBF16, In16>(a, head_dim, stream);
+    return launch_dim<AttBF16>(a, head_dim, stream);
 }
 
 }  // namespace sv

@@ -92,10 +92,14 @@ struct AttBF16 {
 
 // How the caches hold their values: 16 bits each, or 4 (cache4.hpp).
 struct In16 {
-    static constexpr bool kFour = false;
+    static constexpr bool kFour = false, kDirect = false;
 };
 struct In4 {
-    static constexpr bool kFour = true;
+    static constexpr bool kFour = true, kDirect = false;
+};
+// 4 bits, for few rows: the waves take units in turn and stage all of theirs (cache4_direct.hpp).
+struct In4Direct {
+    static constexpr bool kFour = true, kDirect = true;
 };
 
 constexpr int kThreads = 256;
@@ -382,7 +386,9 @@ struct Work {
     int64_t place;              // of its part
     bool whole;                 // it is the whole task, and has no part
     uint32_t at;                // place in the cost behind it
-    uint32_t paged;             // lane l has the place in the caches of this wave's rows of unit `paged` + l
+    // lane l has the place in the caches of this wave's rows of unit `paged` + l (where the waves take units in
+    // turn, of run l % 4 of its unit number l / 4 from there)
+    uint32_t paged;
     uint32_t row_low, row_high;
     uint32_t row_scales;        // in 4 bits: and how far behind it the scales of those rows are, in bytes
     bool poison;                // (one of them would have been on a page that there is not)
@@ -402,7 +408,7 @@ struct Work {
         g.first += g.offset;
         g.end += g.offset;
         poison = g.bad;
-        paged = g.first;
+        paged = g.first + (C::kDirect ? (uint32_t)uniform((int32_t)(threadIdx.x >> 6)) : 0u);
         look_up();
         if constexpr (kKind != kShared) look_behind();
         return true;
@@ -428,10 +434,10 @@ struct Work {
     }
     __device__ __forceinline__ void look_up() {
         const int lane = forget((int)threadIdx.x) & 63, wave = uniform((int32_t)(threadIdx.x >> 6));
-        const uint32_t u = smaller(paged + lane, g.end - 1);
+        const uint32_t u = smaller(paged + (C::kDirect ? lane & ~3 : lane), g.end - 1);
         const bool prefix = in_prefix(u);
         const int32_t* const table = prefix ? a.prefix_table : a.block_table + (int64_t)max(g.b, 0) * a.split.max_pages;
-        const int first = run_start(first_key(u), wave, last_key(prefix));
+        const int first = run_start(first_key(u), C::kDirect ? lane & 3 : wave, last_key(prefix));
         int page = (prefix || !g.bad) ? table[first >> a.split.page_shift] : 0;
         if ((uint32_t)page >= (uint32_t)a.num_pages) {
             page = 0;
@@ -1000,14 +1006,14 @@ __device__ __forceinline__ uint32_t place_in_xcd(uint32_t block, uint32_t groups
 
 // kPrefix and kRows: waves that split the rows of the prefix's tasks (0: there are
 // none, a sequence's tasks begin with it) and of the sequences' own.
-template <class T, class C, int D, int kPrefix, int kRows>
+template <class T, int D, int kPrefix, int kRows>
 __global__ void __launch_bounds__(kThreads, (D > 128 ? 1 : 2)) attend_kernel(AttendArgs a) {
     extern __shared__ __attribute__((aligned(16))) char smem[];
     __shared__ uint32_t wave_sums[4][2];
     __shared__ float wave_stats[4][2][32];
     __shared__ int poison_flag, special_flag;
     const Split& split = a.split;
-    int32_t* const words = (int32_t*)(smem + kTiles<C, D>);
+    int32_t* const words = (int32_t*)(smem + kTiles<In16, D>);
     const Batch batch{words, (uint32_t*)words + split.batch + 1, words + 2 * (split.batch + 1)};
     if (threadIdx.x == 0) poison_flag = special_flag = 0;
     const Totals t = sum_batch(split, batch, wave_sums);
@@ -1019,13 +1025,13 @@ __global__ void __launch_bounds__(kThreads, (D > 128 ? 1 : 2)) attend_kernel(Att
         }
     if constexpr (kPrefix == 0) {
         if (blockIdx.x < t.own.groups)
-            run<T, C, D, kRows, kJoined>(a, t, t.own, batch, place_in_xcd(blockIdx.x, t.own.groups), smem, wave_stats,
+            run<T, In16, D, kRows, kJoined>(a, t, t.own, batch, place_in_xcd(blockIdx.x, t.own.groups), smem, wave_stats,
                                       &poison_flag, &special_flag);
     } else if (blockIdx.x < t.prefix.groups) {
-        run<T, C, D, kPrefix, kShared>(a, t, t.prefix, batch, place_in_xcd(blockIdx.x, t.prefix.groups), smem, wave_stats,
+        run<T, In16, D, kPrefix, kShared>(a, t, t.prefix, batch, place_in_xcd(blockIdx.x, t.prefix.groups), smem, wave_stats,
                                     &poison_flag, &special_flag);
     } else if (blockIdx.x - t.prefix.groups < t.own.groups) {
-        run<T, C, D, kRows, kOwn>(a, t, t.own, batch, blockIdx.x - t.prefix.groups, smem, wave_stats, &poison_flag,
+        run<T, In16, D, kRows, kOwn>(a, t, t.own, batch, blockIdx.x - t.prefix.groups, smem, wave_stats, &poison_flag,
                                &special_flag);
     }
 }
@@ -1298,12 +1304,19 @@ __global__ void __launch_bounds__(kThreads) attend_join_tasks_kernel(AttendArgs 
 template <int D>
 constexpr int kMaxTaskRows = D > 128 ? 64 : 128;
 
-template <class T, class C, int D>
+// Bytes of LDS beside the tiles: the batch's sums.
+inline size_t batch_bytes(const AttendArgs& a) { return 3 * sizeof(int32_t) * ((size_t)a.split.batch + 1); }
+
+// The kernels that join the parts.
+template <class T, int D>
+sv_status_t launch_join(const AttendArgs& a, hipStream_t stream);
+
+template <class T, int D>
 sv_status_t launch(const AttendArgs& a, hipStream_t stream) {
-    const size_t lds = kTiles<C, D> + 3 * sizeof(int32_t) * ((size_t)a.split.batch + 1);
+    const size_t lds = kTiles<In16, D> + batch_bytes(a);
     const uint32_t groups = (uint32_t)a.split.plan.groups;
     auto go = [&](auto prefix, auto own) {
-        hipLaunchKernelGGL((attend_kernel<T, C, D, decltype(prefix)::value, decltype(own)::value>), dim3(groups),
+        hipLaunchKernelGGL((attend_kernel<T, D, decltype(prefix)::value, decltype(own)::value>), dim3(groups),
                            dim3(kThreads), lds, stream, a);
     };
     constexpr std::integral_constant<int, 0> k0{};
@@ -1319,6 +1332,12 @@ sv_status_t launch(const AttendArgs& a, hipStream_t stream) {
         own == 1 ? go(k2, k1) : go(k2, k2);
     else
         own == 1 ? go(k4, k1) : own == 2 ? go(k4, k2) : go(k4, k4);
+    return launch_join<T, D>(a, stream);
+}
+
+template <class T, int D>
+sv_status_t launch_join(const AttendArgs& a, hipStream_t stream) {
+    const uint32_t groups = (uint32_t)a.split.plan.groups;
     if (a.split.plan.joined) {
         if (groups > 1)
             hipLaunchKernelGGL((attend_join_tasks_kernel<T, D>), dim3(groups - 1, a.split.plan.own_rows / kJoinRows),
@@ -1338,14 +1357,14 @@ sv_status_t launch(const AttendArgs& a, hipStream_t stream) {
     return hipGetLastError() == hipSuccess ? SV_OK : SV_ERR_HIP;
 }
 
-template <class T, class C>
+template <class T>
 sv_status_t launch_dim(const AttendArgs& a, int32_t head_dim, hipStream_t stream) {
     switch (head_dim) {
-        case 64: return launch<T, C, 64>(a, stream);
-        case 80: return launch<T, C, 80>(a, stream);
-        case 96: return launch<T, C, 96>(a, stream);
-        case 128: return launch<T, C, 128>(a, stream);
-        default: return launch<T, C, 256>(a, stream);
+        case 64: return launch<T, 64>(a, stream);
+        case 80: return launch<T, 80>(a, stream);
+        case 96: return launch<T, 96>(a, stream);
+        case 128: return launch<T, 128>(a, stream);
+        default: return launch<T, 256>(a, stream);
     }
 }
 

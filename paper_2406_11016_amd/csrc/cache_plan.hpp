@@ -92,6 +92,7 @@ struct AttendPlan {
     int32_t groups;               // workgroups
     int64_t own_parts, rows;      // row places of the parts: of the first own one, of all
     size_t cum_bytes;             // one array of sums over the batch
+    bool own_direct, prefix_direct;  // caches in 4 bits: such tasks go by cache4_direct.hpp
 };
 
 constexpr size_t kTotalsBytes = 256;  // room in the workspace for the split's totals, see cache_split.hpp
@@ -118,6 +119,20 @@ constexpr bool joined_pays(int64_t tasks, int64_t groups, int64_t rows, int64_t 
     return 2 * tasks >= groups && 8 * rows >= 7 * ((rows + tile_rows - 1) / tile_rows * tile_rows);
 }
 
+// Places of the parts, from the rest of the plan.
+inline void place_parts(AttendPlan& p, int32_t batch, int64_t rows, int32_t kv_heads) {
+    if (p.joined) {
+        p.own_parts = 0;
+        p.rows = 2 * (int64_t)p.groups * p.own_rows;
+    } else {
+        const int64_t prefix_tasks = kv_heads * ((batch * rows + p.prefix_rows - 1) / p.prefix_rows);
+        // (chunks of the prefix have at least a workgroup's share of its units, see Totals: at most `groups` tasks more)
+        p.own_parts = (prefix_tasks + 3 * p.groups + 1) * p.prefix_rows;
+        p.rows = p.own_parts + ((int64_t)batch * kv_heads * p.own_tiles + p.groups) * p.own_rows;
+    }
+    p.cum_bytes = (sizeof(int32_t) * ((size_t)batch + 1) + 255) / 256 * 256;
+}
+
 inline AttendPlan attend_plan(int32_t batch, int32_t max_new, int32_t q_heads, int32_t kv_heads, int32_t head_dim,
                               bool prefix) {
     AttendPlan p{};
@@ -129,16 +144,7 @@ inline AttendPlan attend_plan(int32_t batch, int32_t max_new, int32_t q_heads, i
     p.prefix_shift = __builtin_ctz((unsigned)p.prefix_rows);
     p.groups = head_dim > 128 ? 256 : 512;  // what the 256 CUs hold at a time: one of 128 KiB LDS each, or two of 64
     p.joined = !prefix || joined_pays((int64_t)batch * kv_heads * p.own_tiles, p.groups, rows, task_rows(1 << 20, head_dim));
-    if (p.joined) {
-        p.own_parts = 0;
-        p.rows = 2 * (int64_t)p.groups * p.own_rows;
-    } else {
-        const int64_t prefix_tasks = kv_heads * ((batch * rows + p.prefix_rows - 1) / p.prefix_rows);
-        // (chunks of the prefix have at least a workgroup's share of its units, see Totals: at most `groups` tasks more)
-        p.own_parts = (prefix_tasks + 3 * p.groups + 1) * p.prefix_rows;
-        p.rows = p.own_parts + ((int64_t)batch * kv_heads * p.own_tiles + p.groups) * p.own_rows;
-    }
-    p.cum_bytes = (sizeof(int32_t) * ((size_t)batch + 1) + 255) / 256 * 256;
+    place_parts(p, batch, rows, kv_heads);
     return p;
 }
 
@@ -161,26 +167,51 @@ inline bool attend_units_ok(const sv_cache_attend_desc_t& d, const AttendPlan& p
 }
 
 inline size_t attend_workspace_bytes(int32_t batch, int32_t max_new, int32_t q_heads, int32_t kv_heads,
-                                     int32_t head_dim) {
+                                     int32_t head_dim, decltype(&attend_plan) plan = attend_plan) {
     if (!attend_sizes_ok(batch, max_new, q_heads, kv_heads, head_dim)) return 0;
     size_t most = 0;
     for (const bool prefix : {false, true}) {
-        const AttendPlan p = attend_plan(batch, max_new, q_heads, kv_heads, head_dim, prefix);
+        const AttendPlan p = plan(batch, max_new, q_heads, kv_heads, head_dim, prefix);
         const size_t n = 2 * p.cum_bytes + kTotalsBytes + (size_t)p.rows * ((size_t)head_dim + 2) * sizeof(float);
         if (n > most) most = n;
     }
     return (most + 255) / 256 * 256;
 }
 
-// Caches in 4 bits: at head_dim 256 a unit's bytes as they come from memory share the LDS, too.
+// Caches in 4 bits: rows up to which a task's cost is its keys' bytes.
+inline int64_t direct_rows(int32_t head_dim) { return head_dim > 128 ? 16 : 48; }
+
+inline AttendPlan attend4_plan(int32_t batch, int32_t max_new, int32_t q_heads, int32_t kv_heads, int32_t head_dim,
+                               bool prefix) {
+    AttendPlan p = attend_plan(batch, max_new, q_heads, kv_heads, head_dim, prefix);
+    const int64_t rows = (int64_t)max_new * (q_heads / kv_heads), most = direct_rows(head_dim);
+    const auto tile = [](int64_t r) { return r <= 16 ? 16 : r <= 32 ? 32 : 64; };
+    p.own_direct = rows <= most;
+    p.prefix_direct = !p.joined && batch * rows <= most;
+    if (p.own_direct) {
+        p.own_rows = tile(rows);
+        p.own_tiles = 1;
+    } else if (head_dim <= 128 && p.own_rows == 32) {
+        p.own_rows = 64;
+    }
+    if (p.prefix_direct) p.prefix_rows = tile(batch * rows);
+    p.own_shift = __builtin_ctz((unsigned)p.own_rows);
+    p.prefix_shift = __builtin_ctz((unsigned)p.prefix_rows);
+    // (as many as the CUs hold, three of 37 KiB where one kind of few rows is all)
+    if (p.own_direct && p.joined) p.groups = head_dim > 128 ? 512 : p.own_rows == 16 ? 768 : 512;
+    place_parts(p, batch, rows, kv_heads);
+    return p;
+}
+
+// At head_dim 256 a unit's bytes as they come from memory share the LDS, too.
 inline size_t attend4_workspace_bytes(int32_t batch, int32_t max_new, int32_t q_heads, int32_t kv_heads,
                                       int32_t head_dim) {
     if (head_dim > 128 && batch > SV_CACHE4_MAX_BATCH_D256) return 0;
-    return attend_workspace_bytes(batch, max_new, q_heads, kv_heads, head_dim);
+    return attend_workspace_bytes(batch, max_new, q_heads, kv_heads, head_dim, attend4_plan);
 }
 
-template <class CheckCache = decltype(&check_cache)>
-inline sv_status_t check_attend(const sv_cache_attend_desc_t& d, CheckCache check = check_cache) {
+inline sv_status_t check_attend(const sv_cache_attend_desc_t& d, decltype(&check_cache) check = check_cache,
+                                decltype(&attend_plan) plan = attend_plan) {
     if (d.q == nullptr || d.out == nullptr || d.k_cache == nullptr || d.v_cache == nullptr || d.block_table == nullptr ||
         d.lengths == nullptr || d.workspace == nullptr || (d.prefix_len != 0 && d.prefix_table == nullptr))
         return SV_ERR_NULL;
@@ -191,7 +222,7 @@ inline sv_status_t check_attend(const sv_cache_attend_desc_t& d, CheckCache chec
         (int64_t)d.batch * d.max_pages > INT_MAX || (int64_t)d.max_pages * d.page_size > INT_MAX || d.prefix_len < 0 ||
         (int64_t)d.prefix_len + (int64_t)d.max_pages * d.page_size > INT_MAX)
         return SV_ERR_SHAPE;
-    if (!attend_units_ok(d, attend_plan(d.batch, d.max_new, d.q_heads, d.kv_heads, d.head_dim, d.prefix_len > 0)))
+    if (!attend_units_ok(d, plan(d.batch, d.max_new, d.q_heads, d.kv_heads, d.head_dim, d.prefix_len > 0)))
         return SV_ERR_SHAPE;
     // (scale * log2(e) and its inverse have to be finite)
     if (!(d.scale > 1e-30f && d.scale < 1e30f)) return SV_ERR_PARAM;
@@ -200,13 +231,13 @@ inline sv_status_t check_attend(const sv_cache_attend_desc_t& d, CheckCache chec
         !rows_apart(d.out_stride, d.batch, d.max_new, d.q_heads))
         return SV_ERR_PARAM;
     if (!aligned16(d.workspace) ||
-        d.workspace_bytes < attend_workspace_bytes(d.batch, d.max_new, d.q_heads, d.kv_heads, d.head_dim))
+        d.workspace_bytes < attend_workspace_bytes(d.batch, d.max_new, d.q_heads, d.kv_heads, d.head_dim, plan))
         return SV_ERR_WORKSPACE;
     return SV_OK;
 }
 
 inline sv_status_t check_attend4(const sv_cache_attend_desc_t& d) {
-    const sv_status_t st = check_attend(d, check_cache4);
+    const sv_status_t st = check_attend(d, check_cache4, attend4_plan);
     if (st != SV_OK) return st;
     return d.head_dim > 128 && d.batch > SV_CACHE4_MAX_BATCH_D256 ? SV_ERR_SHAPE : SV_OK;
 }
