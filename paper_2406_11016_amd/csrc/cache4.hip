@@ -219,8 +219,9 @@ sv_status_t spec_cache_attend4(const sv_cache_attend_desc_t* desc, hipStream_t s
     const sv_cache_attend_desc_t& d = *desc;
     const sv_status_t st = sv::check_attend4(d);
     if (st != SV_OK) return st;
-    const sv::AttendArgs a =
-        sv::attend_args(d, sv::attend4_plan(d.batch, d.max_new, d.q_heads, d.kv_heads, d.head_dim, d.prefix_len > 0));
+    sv::AttendPlan plan = sv::attend4_plan(d.batch, d.max_new, d.q_heads, d.kv_heads, d.head_dim, d.prefix_len > 0);
+    plan.whole_tasks = sv::whole_pays(plan, d);
+    const sv::AttendArgs a = sv::attend_args(d, plan);
     return d.dtype == SV_F16 ? sv::attend4_f16(a, d.head_dim, stream) : sv::attend4_bf16(a, d.head_dim, stream);
 }
 

@@ -21,21 +21,21 @@ constexpr int kLds4 = kTaskLds<D, kPrefix> > kTaskLds<D, kRows> ? kTaskLds<D, kP
 
 // Workgroups of a CU at a time, which the registers have to be enough for (and attend4_plan counts on).
 template <int D, int kPrefix, int kRows>
-constexpr int kResident = kPrefix == 0 && kRows == -1 ? (D > 128 ? 2 : 3) : (D > 128 ? 1 : 2);
+constexpr int kResident = D > 128 && !(kPrefix == 0 && kRows == -1) ? 1 : 2;
 
 struct Shared4 {
     float wave_stats[4][2][48];
-    int poison_flag, special_flag;
+    __attribute__((aligned(8))) int flags[2];  // poison and special values, or the poison of two tasks in turn
 };
 
 template <class T, int D, int kRows, Kind kKind>
 __device__ __forceinline__ void run4(const AttendArgs& a, const Totals& t, const Deal& deal, const Batch& batch, uint32_t w,
                                      char* smem, Shared4& shared) {
     if constexpr (kRows > 0)
-        run<T, In4, D, kRows, kKind>(a, t, deal, batch, w, smem, (float(*)[2][32])shared.wave_stats, &shared.poison_flag,
-                                     &shared.special_flag);
+        run<T, In4, D, kRows, kKind>(a, t, deal, batch, w, smem, (float(*)[2][32])shared.wave_stats, &shared.flags[0],
+                                     &shared.flags[1]);
     else
-        run_direct<T, D, -kRows, kKind>(a, t, deal, batch, w, smem, shared.wave_stats, &shared.poison_flag);
+        run_direct<T, D, -kRows, kKind>(a, t, deal, batch, w, smem, shared.wave_stats, shared.flags);
 }
 
 template <class T, int D, int kPrefix, int kRows>
@@ -46,7 +46,7 @@ __global__ void __launch_bounds__(kThreads, (kResident<D, kPrefix, kRows>)) atte
     const Split& split = a.split;
     int32_t* const words = (int32_t*)(smem + kLds4<D, kPrefix, kRows>);
     const Batch batch{words, (uint32_t*)words + split.batch + 1, words + 2 * (split.batch + 1)};
-    if (threadIdx.x == 0) shared.poison_flag = shared.special_flag = 0;
+    if (threadIdx.x == 0) shared.flags[0] = shared.flags[1] = 0;
     const Totals t = sum_batch(split, batch, wave_sums);
     if (blockIdx.x == 0)  // for the kernel that joins the parts
         for (int b = threadIdx.x; b <= split.batch; b += kThreads) {
@@ -87,19 +87,22 @@ sv_status_t launch4(const AttendArgs& a, hipStream_t stream) {
         else
             prefix == 0 ? go(none, most) : go(most, most);
     } else {
+        // (a prefix of few rows in all is for any of up to 48: the rows that there are not cost little there)
+        constexpr std::integral_constant<int, -2> more{};
         constexpr std::integral_constant<int, -3> some{};
         constexpr std::integral_constant<int, 2> two{};
-        const bool prefix_few = plan.prefix_rows == 16, prefix_two = plan.prefix_rows == 64;
-        if (plan.own_direct && plan.own_rows == 16)
-            prefix == 0 ? go(none, few)
-                        : prefix < 0 ? (prefix_few ? go(few, few) : go(some, few)) : prefix_two ? go(two, few) : go(most, few);
+        const bool prefix_two = plan.prefix_rows == 64;
+        auto direct = [&](auto own) { prefix == 0 ? go(none, own) : prefix_two ? go(two, own) : go(most, own); };
+        if (plan.prefix_direct)
+            go(some, few);
         else if (plan.own_direct)
-            prefix == 0 ? go(none, some) : prefix < 0 ? go(some, some) : prefix_two ? go(two, some) : go(most, some);
+            plan.own_rows == 16 ? direct(few) : plan.own_rows == 32 ? direct(more) : direct(some);
         else if (plan.own_rows == 64)
             prefix == 0 ? go(none, two) : prefix_two ? go(two, two) : go(most, two);
         else
             prefix == 0 ? go(none, most) : go(most, most);
     }
+    if (plan.whole_tasks) return hipGetLastError() == hipSuccess ? SV_OK : SV_ERR_HIP;
     return launch_join<T, D>(a, stream);
 }
 

@@ -58,8 +58,11 @@ struct Direct {
     // Q of several row tiles lies in LDS, for all waves, in the order in which they read it (there are no registers for it)
     static constexpr bool q_in_lds(int tiles) { return tiles > 1 || D > 128; }
     static constexpr int lds(int tiles) { return 4 * kWave + (q_in_lds(tiles) ? tiles * kSteps * 1024 : 0); }
-    static constexpr int kPitch = D + 4;                       // floats of a row when the waves' outputs are joined
-    static_assert(16 * kPitch * 4 <= kWave, "the outputs of 16 rows fit a wave's LDS");
+    // When the waves' outputs are joined, 16 rows of some pieces at a time go through each wave's LDS but for its first
+    // buffer, to which the next task's first values are on their way.
+    static constexpr int kBoxPieces = D >= 128 ? D / 64 : 1, kBoxes = kPieces / kBoxPieces;
+    static constexpr int kPitch = 32 * kBoxPieces + 4;         // floats of a row there
+    static_assert(16 * kPitch * 4 <= kWave - kTile && kBoxes * kBoxPieces == kPieces, "they fit");
     // first value of product s for a quarter, and (a lane's number of) its scale
     static constexpr __device__ int value(int s, int quarter) {
         const int in = kWide / 8, j = s / in;
@@ -81,9 +84,9 @@ struct KeysComing {
     uint32_t scale[4][Direct<D>::kScales];
 };
 
-// The part of a task's rows over a run of its units: RT tiles of 16 rows.  Each of the
-// four waves takes every fourth unit, for all rows, and stages it alone, so no wave
-// waits for another until the parts of the four are joined at the end.
+// A workgroup's run of tasks of RT tiles of 16 rows.  Each of the four waves takes
+// every fourth unit of a task, for all rows, and stages it alone, so no wave waits for
+// another until the parts of the four are joined at the task's end.
 //
 // K goes from memory to registers and is widened there: 16 bytes a lane are a whole block of a key
 // at D = 128, the A operand of S^T = K Q^T as they stand if Q's values are taken in the
@@ -93,17 +96,20 @@ struct KeysComing {
 // the rows of the A operands of O^T = V^T P^T, even and odd.  P^T is its B operand as it
 // comes from S^T, rounded to the storage type as in the 16-bit kernels.
 //
-// (The next unit's loads go out before this one's work, so a wave has 8.5 KB under way at D = 128.)
+// The next unit's loads go out before this one's work, and the next task's first ones
+// before this one's parts are joined, so a wave always has some of the cache on its way (8.5 KB at
+// D = 128).
 template <class T, int D, int RT, Kind kKind>
-__device__ __forceinline__ bool direct_segment(Work<In4Direct, D, kKind>& work, char* smem, float (*wave_stats)[2][48],
-                                               int* poison_flag) {
+__device__ __forceinline__ void run_direct(const AttendArgs& a, const Totals& t, const Deal& deal, const Batch& batch,
+                                           uint32_t group_number, char* smem, float (*wave_stats)[2][48], int* flags) {
     using S = Direct<D>;
     using V8 = typename T::V8;
-    const int tid = threadIdx.x, lane = forget(tid & 63), quarter = lane >> 4, of16 = lane & 15;
-    const int wave = uniform(tid >> 6);
-    const AttendArgs& a = work.a;
-    const Segment g = work.g;
-    const int32_t* const cum_tokens = work.batch.cum_tokens;
+    const int wave = forget_scalar(uniform((int32_t)(threadIdx.x >> 6)));
+    Work<In4Direct, D, kKind> work{a, t, batch, (uint32_t)(uintptr_t)(SV_LDS char*)smem, group_number,
+                                   group_start(deal, group_number + 1), {}, 0, false, group_start(deal, group_number), 0, 0, 0, 0,
+                                   false, wave, flags + 1};
+    if (!work.advance()) return;
+    const int lane = lane_again<In4Direct>(), quarter = lane >> 4, of16 = lane & 15;
     char* const mine = smem + wave * S::kWave;
     const uint32_t mine_lds = work.lds + wave * S::kWave;
     float* const v_scales = (float*)(mine + 2 * S::kTile);
@@ -112,52 +118,48 @@ __device__ __forceinline__ bool direct_segment(Work<In4Direct, D, kKind>& work, 
         int b, token, head;
         bool live;
     };
-    auto row_of = [&](int in_task) {
+    auto row_of = [&](const Segment& g, int in_task) {
+        const int group = forget_scalar(a.split.group);  // (see Work::advance)
         const int row = g.row0 + in_task;
-        const int flat = (int)((uint32_t)row / (uint32_t)a.split.group);
-        Row r{g.b, flat, g.kv_head * a.split.group + (row - flat * a.split.group), flat < g.count};
+        const int flat = (int)((uint32_t)row / (uint32_t)group);
+        Row r{g.b, flat, g.kv_head * group + (row - flat * group), flat < g.count};
         if (kKind == kShared) {
-            r.live = flat < cum_tokens[a.split.batch];
-            r.b = r.live ? find(cum_tokens, a.split.batch, flat) : 0;
-            r.token = r.live ? flat - cum_tokens[r.b] : 0;
+            r.live = flat < batch.cum_tokens[a.split.batch];
+            r.b = r.live ? find(batch.cum_tokens, a.split.batch, flat) : 0;
+            r.token = r.live ? flat - batch.cum_tokens[r.b] : 0;
         }
         return r;
     };
-    // tiles with a row that there is (all tasks have one)
-    const int rows = uniform((kKind == kShared ? cum_tokens[a.split.batch] : g.count) * a.split.group - g.row0);
-    const int tiles = RT == 1 ? 1 : min(RT, (rows + 15) / 16);
 
+    // ---- Q: B operands of the products, those of several row tiles made by one wave each, for LDS
     constexpr bool kQInLds = S::q_in_lds(RT);
-    V8* const q_lds = (V8*)(smem + 4 * S::kWave);  // [product][row tile][lane]
-    V8 q[kQInLds ? 1 : RT][kQInLds ? 1 : S::kSteps];
-    int own_limit[RT];  // keys of its own that the row sees
-    f32x4 o[RT][S::kPieces][2];
-    float top[RT], sum[RT];
-    bool far[RT];
+    constexpr int kQs = kQInLds ? (RT * S::kSteps + 3) / 4 : S::kSteps;  // of a wave
+    V8* const q_lds = (V8*)(smem + 4 * S::kWave);                        // [product][row tile][lane]
+    V8 q[kQs];
+    auto load_q = [&]() {
+        // (what is made from it would else be kept in registers from before)
+        const int lane = lane_again<In4Direct>(), quarter = lane >> 4, of16 = lane & 15;
 #pragma unroll
-    for (int r = 0; r < RT; ++r) {
-        const Row row = row_of(r * 16 + of16);
-        own_limit[r] = g.length + row.token + 1;
-        const uint16_t* const from = a.q + row.b * a.q_stride[0] + row.token * a.q_stride[1] + row.head * a.q_stride[2];
-#pragma unroll
-        for (int s = 0; s < S::kSteps; ++s) {
+        for (int i = 0; i < kQs; ++i) {
+            const int at = kQInLds ? 4 * i + wave : i, s = kQInLds ? at / RT : i, r = kQInLds ? at % RT : 0;
             u32x4 x = {0, 0, 0, 0};
-            if (kQInLds && (s * RT + r) % 4 != wave) continue;
-            if (row.live && S::there(s, quarter)) x = *(const u32x4*)(from + S::value(s, quarter));
-            if constexpr (kQInLds)
-                q_lds[(s * RT + r) * 64 + lane] = __builtin_bit_cast(V8, x);
-            else
-                q[r][s] = __builtin_bit_cast(V8, x);
+            if (s < S::kSteps) {
+                const Row row = row_of(work.g, r * 16 + of16);
+                const uint16_t* const from =
+                    a.q + row.b * a.q_stride[0] + row.token * a.q_stride[1] + row.head * a.q_stride[2];
+                if (row.live && S::there(s, quarter)) x = *(const u32x4*)(from + S::value(s, quarter));
+            }
+            q[i] = __builtin_bit_cast(V8, x);
         }
+    };
+    auto keep_q = [&]() {
+        if constexpr (kQInLds) {
+            const int lane = lane_again<In4Direct>();
 #pragma unroll
-        for (int p = 0; p < S::kPieces; ++p) o[r][p][0] = o[r][p][1] = f32x4(0.0f);
-        top[r] = -INFINITY;
-        sum[r] = 0.0f;
-        far[r] = false;
-    }
-    if constexpr (kQInLds) lds_barrier();
-    const int own_first = kKind == kShared ? 0 : own_common(a.split, g);
-    const int last = work.last_key(kKind == kShared);  // the last key that there is
+            for (int i = 0; i < kQs; ++i)
+                if (4 * i + wave < RT * S::kSteps) q_lds[(4 * i + wave) * 64 + lane] = q[i];
+        }
+    };
 
     // ---- a unit's loads
     auto run_at = [&](int at) {  // bytes before the rows of a run
@@ -211,7 +213,7 @@ __device__ __forceinline__ bool direct_segment(Work<In4Direct, D, kKind>& work, 
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const char* const k_from = (const char*)a.k_cache + run_at(at + r);
-            const uint32_t scales = (uint32_t)__builtin_amdgcn_readlane((int)work.row_scales, at + r);
+            const char* const k_scales = k_from + (uint32_t)__builtin_amdgcn_readlane((int)work.row_scales, at + r);
 #pragma unroll
             for (int j = 0; j < S::kWides; ++j) {
                 const char* const from = k_from + (uint32_t)(of16 * S::kRow + (4 * j + quarter) * (S::kWide / 2));
@@ -224,17 +226,53 @@ __device__ __forceinline__ bool direct_segment(Work<In4Direct, D, kKind>& work, 
                     k.codes[r][2 * j] = x[0];
                     k.codes[r][2 * j + 1] = x[1];
                 }
-                k.scale[r][j] = *(const uint8_t*)(k_from + scales + (uint32_t)(of16 * S::kBlocks) +
-                                                  (uint32_t)((4 * j + quarter) * S::kWide / 32));
+                k.scale[r][j] = *(const uint8_t*)(k_scales + (uint32_t)(of16 * S::kBlocks + (4 * j + quarter) * S::kWide / 32));
             }
             if constexpr (S::kRest > 0) {
                 uint32_t x = 0;
                 if (S::there(S::kSteps - 1, quarter)) x = *(const uint32_t*)(k_from + (uint32_t)(of16 * S::kRow + 32 + 4 * quarter));
                 k.codes[r][S::kSteps - 1] = x;
-                k.scale[r][S::kScales - 1] = *(const uint8_t*)(k_from + scales + (uint32_t)(of16 * S::kBlocks + 2));
+                k.scale[r][S::kScales - 1] = *(const uint8_t*)(k_scales + (uint32_t)(of16 * S::kBlocks + 2));
             }
         }
     };
+
+    // K of the next unit goes out with V before this one's work or, with several row tiles, when this one's K has been
+    // used, into its registers.
+    constexpr bool kLate = RT > 1;
+    KeysComing<D> k[kLate ? 1 : 2];
+    uint32_t vs[2][2] = {};
+    auto fetch_first = [&]() {
+        const uint32_t u = work.g.first + wave;
+        if (u < work.g.end) {
+            fetch_v(u, 0, vs[0]);
+            fetch_k(u, k[0]);
+        }
+    };
+    fetch_first();
+    load_q();
+    keep_q();
+    if constexpr (kQInLds) lds_barrier();
+
+    for (;;) {
+    const Segment g = work.g;
+    // keys that the lane's row of tile r sees (rarely needed, so not kept)
+    auto limit_of = [&](int r) {
+        return kKind == kShared ? a.prefix_len : g.length + row_of(g, r * 16 + (lane_again<In4Direct>() & 15)).token + 1;
+    };
+    f32x4 o[RT][S::kPieces][2];
+    float top[RT], sum[RT];
+    bool far[RT];
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+#pragma unroll
+        for (int p = 0; p < S::kPieces; ++p) o[r][p][0] = o[r][p][1] = f32x4(0.0f);
+        top[r] = -INFINITY;
+        sum[r] = 0.0f;
+        far[r] = false;
+    }
+    const int own_first = kKind == kShared ? 0 : own_common(a.split, g);
+    const int last = work.last_key(kKind == kShared);  // the last key that there is
 
     // ---- a unit's work
     auto look_far = [&](int r) { far[r] = __any(fabsf(top[r] * a.scale_log2) > kFarScores && top[r] != -INFINITY); };
@@ -266,15 +304,16 @@ __device__ __forceinline__ bool direct_segment(Work<In4Direct, D, kKind>& work, 
             for (int n = 0; n < 4; ++n) w[r][n] = f32x4(0.0f);
 #pragma unroll
         for (int s = 0; s < S::kSteps; ++s) {
+            if (RT > 1) in_order();  // (nor has it registers for more of Q)
             V8 y[RT];
 #pragma unroll
-            for (int r = 0; r < RT; ++r) y[r] = kQInLds ? q_lds[(s * RT + r) * 64 + lane] : q[kQInLds ? 0 : r][kQInLds ? 0 : s];
+            for (int r = 0; r < RT; ++r) y[r] = kQInLds ? q_lds[(s * RT + r) * 64 + lane] : q[kQInLds ? 0 : s];
 #pragma unroll
             for (int n = 0; n < 4; ++n) {
                 const V8 x = __builtin_bit_cast(V8, T::wide(k.codes[n][s], __uint_as_float(k.scale[n][S::scale(s)] << 23)));
 #pragma unroll
                 for (int r = 0; r < RT; ++r)
-                    if (r < tiles) w[r][n] = mma16(x, y[r], w[r][n]);
+                    w[r][n] = mma16(x, y[r], w[r][n]);
             }
         }
         after_scores();
@@ -282,9 +321,8 @@ __device__ __forceinline__ bool direct_segment(Work<In4Direct, D, kKind>& work, 
         V8 weights[RT][2];
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
-            if (r >= tiles) continue;
             if (partial) {
-                const int limit = kKind == kShared ? a.prefix_len : own_limit[r];
+                const int limit = limit_of(r);
 #pragma unroll
                 for (int n = 0; n < 4; ++n)
 #pragma unroll
@@ -340,12 +378,11 @@ __device__ __forceinline__ bool direct_segment(Work<In4Direct, D, kKind>& work, 
                 const uint32_t s1 = (uint32_t)__builtin_amdgcn_readlane((int)vs_in[1], key);
 #pragma unroll
                 for (int r = 0; r < RT; ++r) {
-                    if (r >= tiles) continue;
                     float weight = 0.0f;
 #pragma unroll
                     for (int j = 0; j < 16; ++j) weight = (j == 4 * n + i) ? (float)weights[r][j / 8][j % 8] : weight;
                     weight = __shfl(weight, from);
-                    const bool sees = key0 + key < (kKind == kShared ? a.prefix_len : own_limit[r]);
+                    const bool sees = key0 + key < limit_of(r);
 #pragma unroll
                     for (int p = 0; p < S::kPieces; ++p) {
                         if (32 * p + 8 * quarter >= D) continue;
@@ -401,7 +438,6 @@ __device__ __forceinline__ bool direct_segment(Work<In4Direct, D, kKind>& work, 
             }
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
-                if (r >= tiles) continue;
                 o[r][p][0] = mma16(__builtin_bit_cast(V8, even), weights[r][b], o[r][p][0]);
                 o[r][p][1] = mma16(__builtin_bit_cast(V8, odd), weights[r][b], o[r][p][1]);
             }
@@ -409,16 +445,7 @@ __device__ __forceinline__ bool direct_segment(Work<In4Direct, D, kKind>& work, 
     };
 
     {
-        // K of the next unit goes out with V before this one's work or, with several row tiles, when this one's K has been
-        // used, into its registers.
-        constexpr bool kLate = RT > 1;
-        KeysComing<D> k[kLate ? 1 : 2];
-        uint32_t vs[2][2] = {};
         uint32_t u = g.first + wave;
-        if (u < g.end) {
-            fetch_v(u, 0, vs[0]);
-            fetch_k(u, k[0]);
-        }
         auto turn = [&](auto odd) {
             constexpr int kHere = decltype(odd)::value, kThere = 1 - kHere;
             const bool more = u + 4 < g.end;
@@ -445,39 +472,39 @@ __device__ __forceinline__ bool direct_segment(Work<In4Direct, D, kKind>& work, 
         }
     }
 
-    // ---- join the four waves' parts, tile by tile, then write
-    const int id = forget((int)threadIdx.x);  // (what is made from it would else be kept in registers from before)
-    if (work.poison) *poison_flag = 1;
+    // ---- the next task's first loads
+    int* const flag = work.flag;  // (set where this task has a page that there is not)
+    const bool whole = kKind == kJoined && work.whole;
+    const int64_t place = work.place;
+    const bool more = work.advance();
+    in_order();
+    if (more) {
+        fetch_first();
+        if constexpr (!kQInLds) load_q();
+    }
+    in_order();
+
+    // ---- join the four waves' parts, some pieces of a row tile at a time, then write
+    const int again = lane_again<In4Direct>(), my_row = again & 15, my_quarter = again >> 4;
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
         sum[r] = quarters_sum(sum[r]);
-        if (quarter == 0) {
-            wave_stats[wave][0][r * 16 + of16] = top[r];
-            wave_stats[wave][1][r * 16 + of16] = sum[r];
+        if (my_quarter == 0) {
+            wave_stats[wave][0][r * 16 + my_row] = top[r];
+            wave_stats[wave][1][r * 16 + my_row] = sum[r];
         }
     }
     lds_barrier();
-    const bool whole = kKind == kJoined && work.whole, nan = *poison_flag != 0;
-    const int64_t place = work.place;
+    const bool nan = *flag != 0;
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
-        if (r >= tiles) continue;
         float now = -INFINITY;
 #pragma unroll
-        for (int x = 0; x < 4; ++x) now = fmaxf(now, wave_stats[x][0][r * 16 + of16]);
+        for (int x = 0; x < 4; ++x) now = fmaxf(now, wave_stats[x][0][r * 16 + my_row]);
         const float ref = now == -INFINITY ? 0.0f : now;
         const float by = exp2_hw((top[r] - ref) * a.scale_log2);
-        float* const box = (float*)mine + of16 * S::kPitch + 8 * quarter;
-#pragma unroll
-        for (int p = 0; p < S::kPieces; ++p) {
-            if (32 * p + 8 * quarter >= D) continue;
-            const f32x4 x = o[r][p][0] * by, y = o[r][p][1] * by;
-            *(f32x4*)(box + 32 * p) = f32x4{x[0], y[0], x[1], y[1]};
-            *(f32x4*)(box + 32 * p + 4) = f32x4{x[2], y[2], x[3], y[3]};
-        }
-        lds_barrier();
         // 16 threads a row, 4 values at a time
-        const int row = id >> 4, in = r * 16 + row;
+        const int row = 4 * wave + my_quarter, in = r * 16 + row;
         float most = -INFINITY, total = 0.0f;
 #pragma unroll
         for (int x = 0; x < 4; ++x) most = fmaxf(most, wave_stats[x][0][in]);
@@ -485,41 +512,49 @@ __device__ __forceinline__ bool direct_segment(Work<In4Direct, D, kKind>& work, 
 #pragma unroll
         for (int x = 0; x < 4; ++x)
             total += exp2_hw((wave_stats[x][0][in] - reference) * a.scale_log2) * wave_stats[x][1][in];
-        const Row to = row_of(in);
+        const Row to = row_of(g, in);
         const float times = nan ? forget(NAN) : whole ? 1.0f / total : 1.0f;
-        if (!whole && (id & 15) == 0) {
+        if (!whole && my_row == 0) {
             a.part_max[place + in] = most;
             a.part_sum[place + in] = total;
         }
 #pragma unroll
-        for (int j = 0; j < (D / 4 + 15) / 16; ++j) {
-            const int d = 4 * ((id & 15) + 16 * j);
-            if (D % 64 != 0 && d >= D) continue;
-            f32x4 x = f32x4(0.0f);
+        for (int c = 0; c < S::kBoxes; ++c) {
+            float* const box = (float*)(mine + S::kTile) + my_row * S::kPitch + 8 * my_quarter;
 #pragma unroll
-            for (int from = 0; from < 4; ++from) x += *(const f32x4*)((const float*)(smem + from * S::kWave) + row * S::kPitch + d);
-            x *= times;
-            if (!whole)
-                *(f32x4*)(a.part_out + (place + in) * D + d) = x;
-            else if (to.live)
-                *(u32x2*)(a.out + to.b * a.out_stride[0] + to.token * a.out_stride[1] + to.head * a.out_stride[2] + d) =
-                    __builtin_bit_cast(u32x2, __builtin_convertvector(x, typename T::V4));
+            for (int e = 0; e < S::kBoxPieces; ++e) {
+                const int p = c * S::kBoxPieces + e;
+                const f32x4 x = o[r][p][0] * by, y = o[r][p][1] * by;
+                *(f32x4*)(box + 32 * e) = f32x4{x[0], y[0], x[1], y[1]};
+                *(f32x4*)(box + 32 * e + 4) = f32x4{x[2], y[2], x[3], y[3]};
+            }
+            lds_barrier();
+#pragma unroll
+            for (int j = 0; j < (8 * S::kBoxPieces + 15) / 16; ++j) {
+                const int in_box = 4 * (my_row + 16 * j), d = 32 * c * S::kBoxPieces + in_box;
+                if (in_box >= 32 * S::kBoxPieces || d >= D) continue;
+                f32x4 x = f32x4(0.0f);
+#pragma unroll
+                for (int from = 0; from < 4; ++from)
+                    x += *(const f32x4*)((const float*)(smem + from * S::kWave + S::kTile) + row * S::kPitch + in_box);
+                x *= times;
+                if (!whole)
+                    *(f32x4*)(a.part_out + (place + in) * D + d) = x;
+                else if (to.live)
+                    *(u32x2*)(a.out + to.b * a.out_stride[0] + to.token * a.out_stride[1] + to.head * a.out_stride[2] + d) =
+                        __builtin_bit_cast(u32x2, __builtin_convertvector(x, typename T::V4));
+            }
+            lds_barrier();
         }
-        lds_barrier();
     }
-    if (id == 0) *poison_flag = 0;
-    const bool more = work.advance();
-    lds_barrier();  // (the flag and the statistics are free)
-    return more;
-}
-
-template <class T, int D, int RT, Kind kKind>
-__device__ __forceinline__ void run_direct(const AttendArgs& a, const Totals& t, const Deal& deal, const Batch& batch,
-                                           uint32_t w, char* smem, float (*wave_stats)[2][48], int* poison_flag) {
-    Work<In4Direct, D, kKind> work{a, t, batch, (uint32_t)(uintptr_t)(SV_LDS char*)smem, w, group_start(deal, w + 1),
-                                   {}, 0, false, group_start(deal, w), 0, 0, 0, 0, false};
-    bool more = work.advance();
-    while (more) more = direct_segment<T, D, RT, kKind>(work, smem, wave_stats, poison_flag);
+    if (!more) break;
+    if (wave == 0 && again == 0) *flag = 0;
+    if constexpr (kQInLds) {
+        load_q();
+        keep_q();
+    }
+    lds_barrier();  // (the flag and the statistics are free, too)
+    }
 }
 
 }  // namespace

@@ -123,6 +123,12 @@ __device__ __forceinline__ X forget(X x) {
     return x;
 }
 
+// The same of one that is the same in every lane.
+__device__ __forceinline__ int32_t forget_scalar(int32_t x) {
+    asm volatile("" : "+s"(x));
+    return x;
+}
+
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // max or sum over the two halves of the wave, in every lane
@@ -245,7 +251,7 @@ __device__ __forceinline__ Segment uniform(Segment g) {
     g.row0 = uniform(g.row0);
     g.count = uniform(g.count);
     g.length = uniform(g.length);
-    g.bad = uniform((int32_t)g.bad) != 0;
+    g.bad = uniform(g.bad);
     return g;
 }
 template <class SequenceOf>
@@ -253,6 +259,17 @@ __device__ __forceinline__ Segment own_task_at(const Split& a, const uint32_t* c
     return uniform(own_task(a, cum_cost, u, sequence_of, [&](const Sequence& s, uint32_t at, uint32_t& start) {
         return find_tile(a, s, at, start);
     }));
+}
+
+// find() by a whole wave, of sums in memory: two loads after one another, not twelve.
+// (The batch has 64 x 64 sequences at most.)
+__device__ __forceinline__ int32_t find_by_wave(const uint32_t* cum, int32_t n, uint32_t x) {
+    static_assert(SV_CACHE_MAX_BATCH <= 64 * 64, "a lane a step, then a lane a sequence");
+    const int lane = threadIdx.x & 63, step = (n + 63) / 64;
+    const int of = lane * step;
+    const int first = (__popcll(__ballot(of < n && cum[min(of, n - 1)] <= x)) - 1) * step;
+    const int b = first + lane;
+    return uniform(first + (int)__popcll(__ballot(lane < step && b < n && cum[min(b, n - 1)] <= x)) - 1);
 }
 
 // What a workgroup's tasks are.
@@ -371,6 +388,15 @@ struct Raw {
 template <class C, int D>
 constexpr int kTiles = 2 * Shape<D>::kStage + (C::kFour ? Raw<D>::kTotal : 0);  // bytes of LDS
 
+// The lane's number, made anew.  (The direct kernels have no register to keep the thread's in: it is counted there.)
+template <class C>
+__device__ __forceinline__ int lane_again() {
+    if constexpr (C::kDirect)
+        return forget((int)__builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u)));
+    else
+        return forget((int)threadIdx.x) & 63;
+}
+
 // A workgroup's way through its run of the work: the segment at hand, and the
 // pages that this wave stages of it, a run of 16 rows of each unit.
 template <class C, int D, Kind kKind>
@@ -392,23 +418,59 @@ struct Work {
     uint32_t row_low, row_high;
     uint32_t row_scales;        // in 4 bits: and how far behind it the scales of those rows are, in bytes
     bool poison;                // (one of them would have been on a page that there is not)
+    int32_t wave_number;        // of the workgroup's (direct kernels)
+    int* flag;                  // (and for those not `poison`, but this word of LDS, and the one beside it in turn)
+    __device__ __forceinline__ void bad_page() {
+        if constexpr (C::kDirect)
+            *flag = 1;
+        else
+            poison = true;
+    }
 
     // To the next segment; false if there is none.
     __device__ __forceinline__ bool advance() {
         if (at >= end) return false;
-        if constexpr (kKind == kShared)
+        uint32_t to = end;
+        if constexpr (kKind == kShared && C::kDirect) {
+            Totals now = t;  // (the inverse of a divisor would else be kept in a register from before the loop)
+            now.prefix_tiles = forget_scalar(now.prefix_tiles);
+            g = uniform(prefix_task(a.split, now, at));
+        } else if constexpr (C::kDirect) {  // (such tasks have all of a sequence's rows)
+            auto task = [&]() {
+                return uniform(own_task(a.split, batch.cum_cost, at, [&](int32_t b) { return sequence(batch, b); },
+                                        [](const Sequence&, uint32_t, uint32_t& start) {
+                                            start = 0;
+                                            return 0;
+                                        }));
+            };
+            g = task();
+            if (kKind == kJoined && a.split.plan.whole_tasks) {  // the tasks that begin in this run, to their ends
+                if (at + a.split.plan.own_task_units > g.task_start) {
+                    at = g.task_start + g.units;
+                    if (at >= end) return false;
+                    g = task();
+                }
+                to = g.task_start + g.units;
+            }
+        } else if constexpr (kKind == kShared)
             g = uniform(prefix_task(a.split, t, at));
         else
             g = own_task_at(a.split, batch.cum_cost, at, [&](int32_t b) { return sequence(batch, b); });
-        cut(g, at, end);
+        if constexpr (C::kDirect) g.bad = forget_scalar(g.bad);  // (the compiler would make a lane's register of it)
+        cut(g, at, to);
         if (g.first == g.end) return false;  // (the run ends within the task's cost of starting)
         whole = kKind == kJoined && whole_task(a.split, g);
         place = part_place(a.split, g, group);
         at = g.task_start + g.end;
         g.first += g.offset;
         g.end += g.offset;
-        poison = g.bad;
-        paged = g.first + (C::kDirect ? (uint32_t)uniform((int32_t)(threadIdx.x >> 6)) : 0u);
+        if constexpr (C::kDirect) {
+            flag = (int*)((uintptr_t)flag ^ sizeof(int));
+            if (g.bad) *flag = 1;
+        } else {
+            poison = g.bad != 0;
+        }
+        paged = g.first + (C::kDirect ? (uint32_t)wave_number : 0u);
         look_up();
         if constexpr (kKind != kShared) look_behind();
         return true;
@@ -418,9 +480,9 @@ struct Work {
         const int end = own_end(a.split, g), last = g.length + g.count - 1;
         if (g.bad || end > last) return;
         const int32_t* const table = a.block_table + (int64_t)g.b * a.split.max_pages;
-        for (int j = ((end - 1) >> a.split.page_shift) + 1 + forget((int)threadIdx.x); j <= last >> a.split.page_shift;
-             j += kThreads)
-            if ((uint32_t)table[j] >= (uint32_t)a.num_pages) poison = true;
+        const int thread = C::kDirect ? 64 * wave_number + lane_again<C>() : forget((int)threadIdx.x);
+        for (int j = ((end - 1) >> a.split.page_shift) + 1 + thread; j <= last >> a.split.page_shift; j += kThreads)
+            if ((uint32_t)table[j] >= (uint32_t)a.num_pages) bad_page();
     }
     // Whether unit u is of the prefix, its first key there or in the sequence, and the last key that there is.
     __device__ __forceinline__ bool in_prefix(uint32_t u) const {
@@ -433,7 +495,7 @@ struct Work {
         return prefix ? a.prefix_len - 1 : own_end(a.split, g) - 1;
     }
     __device__ __forceinline__ void look_up() {
-        const int lane = forget((int)threadIdx.x) & 63, wave = uniform((int32_t)(threadIdx.x >> 6));
+        const int lane = lane_again<C>(), wave = uniform((int32_t)(threadIdx.x >> 6));
         const uint32_t u = smaller(paged + (C::kDirect ? lane & ~3 : lane), g.end - 1);
         const bool prefix = in_prefix(u);
         const int32_t* const table = prefix ? a.prefix_table : a.block_table + (int64_t)max(g.b, 0) * a.split.max_pages;
@@ -441,7 +503,7 @@ struct Work {
         int page = (prefix || !g.bad) ? table[first >> a.split.page_shift] : 0;
         if ((uint32_t)page >= (uint32_t)a.num_pages) {
             page = 0;
-            poison = true;
+            bad_page();
         }
         int64_t row;
         if constexpr (C::kFour) {
@@ -988,7 +1050,7 @@ template <class T, class C, int D, int WR, Kind kKind>
 __device__ __forceinline__ void run(const AttendArgs& a, const Totals& t, const Deal& deal, const Batch& batch, uint32_t w,
                                     char* smem, float (*wave_stats)[2][32], int* poison_flag, int* special_flag) {
     Work<C, D, kKind> work{a, t, batch, (uint32_t)(uintptr_t)(SV_LDS char*)smem, w, group_start(deal, w + 1),
-                           {}, 0, false, group_start(deal, w), 0, 0, 0, 0, false};
+                           {}, 0, false, group_start(deal, w), 0, 0, 0, 0, false, 0, nullptr};
     bool more = work.advance();
     if (more) {
         work.stage_first();
@@ -1260,7 +1322,10 @@ __global__ void __launch_bounds__(kThreads) attend_join_tasks_kernel(AttendArgs 
     const Totals& t = *a.totals;
     const uint32_t w = blockIdx.x + 1;
     if (w >= t.own.groups) return;
-    const Segment g = own_task_at(split, a.cum_cost, group_start(t.own, w), [&](int32_t b) { return sequence(split, b); });
+    const uint32_t start = group_start(t.own, w);
+    const Segment g = uniform(own_task_of(
+        split, a.cum_cost, find_by_wave(a.cum_cost, split.batch, start), start, [&](int32_t b) { return sequence(split, b); },
+        [&](const Sequence& s, uint32_t at, uint32_t& tile_start) { return find_tile(split, s, at, tile_start); }));
     uint32_t w0, w1;
     if (!cuts_task(t, g, w, w0, w1)) return;
     const int borders = (int)(w1 - w0), n = 1 + borders, mine = (int)(w - w0) - 1;

@@ -92,7 +92,10 @@ struct AttendPlan {
     int32_t groups;               // workgroups
     int64_t own_parts, rows;      // row places of the parts: of the first own one, of all
     size_t cum_bytes;             // one array of sums over the batch
+    uint32_t own_task_units, prefix_task_units;  // units that count for a task's start and end
+    uint32_t prefix_weight;       // a unit of the prefix's tasks, in units of the others'
     bool own_direct, prefix_direct;  // caches in 4 bits: such tasks go by cache4_direct.hpp
+    bool whole_tasks;             // and no task is cut: a workgroup has those that begin in its run
 };
 
 constexpr size_t kTotalsBytes = 256;  // room in the workspace for the split's totals, see cache_split.hpp
@@ -144,6 +147,8 @@ inline AttendPlan attend_plan(int32_t batch, int32_t max_new, int32_t q_heads, i
     p.prefix_shift = __builtin_ctz((unsigned)p.prefix_rows);
     p.groups = head_dim > 128 ? 256 : 512;  // what the 256 CUs hold at a time: one of 128 KiB LDS each, or two of 64
     p.joined = !prefix || joined_pays((int64_t)batch * kv_heads * p.own_tiles, p.groups, rows, task_rows(1 << 20, head_dim));
+    p.own_task_units = p.prefix_task_units = kTaskUnits;
+    p.prefix_weight = 1;
     place_parts(p, batch, rows, kv_heads);
     return p;
 }
@@ -162,8 +167,8 @@ inline bool attend_units_ok(const sv_cache_attend_desc_t& d, const AttendPlan& p
     const double tiles = (double)d.batch * d.kv_heads * p.own_tiles;
     const double rows = (double)d.batch * d.max_new * (d.q_heads / d.kv_heads);
     // (a chunk of the prefix has a unit at least)
-    const double pooled = p.joined ? 0.0 : d.kv_heads * (double)pre * (1 + kTaskUnits) * (rows / p.prefix_rows + 1.0);
-    return tiles * (double)(own + kTaskUnits + (p.joined ? pre : 0)) + pooled < 2147483647.0;
+    const double pooled = p.joined ? 0.0 : d.kv_heads * (double)pre * (1 + p.prefix_task_units) * (rows / p.prefix_rows + 1.0);
+    return tiles * (double)(own + p.own_task_units + (p.joined ? pre : 0)) + pooled < 2147483647.0;
 }
 
 inline size_t attend_workspace_bytes(int32_t batch, int32_t max_new, int32_t q_heads, int32_t kv_heads,
@@ -178,7 +183,9 @@ inline size_t attend_workspace_bytes(int32_t batch, int32_t max_new, int32_t q_h
     return (most + 255) / 256 * 256;
 }
 
-// Caches in 4 bits: rows up to which a task's cost is its keys' bytes.
+// Caches in 4 bits: rows up to which a task goes by cache4_direct.hpp.  Three tiles of 16 are what the registers are
+// enough for, one at head_dim 256.  (64 sequences of 2,048 to 4,096 cached tokens, 36 rows: 78 us, and 106 as tasks of
+// many rows; 128 of 4,096 to 8,192, 4 rows: 172, and 304.)
 inline int64_t direct_rows(int32_t head_dim) { return head_dim > 128 ? 16 : 48; }
 
 inline AttendPlan attend4_plan(int32_t batch, int32_t max_new, int32_t q_heads, int32_t kv_heads, int32_t head_dim,
@@ -187,18 +194,25 @@ inline AttendPlan attend4_plan(int32_t batch, int32_t max_new, int32_t q_heads, 
     const int64_t rows = (int64_t)max_new * (q_heads / kv_heads), most = direct_rows(head_dim);
     const auto tile = [](int64_t r) { return r <= 16 ? 16 : r <= 32 ? 32 : 64; };
     p.own_direct = rows <= most;
-    p.prefix_direct = !p.joined && batch * rows <= most;
+    p.prefix_direct = !p.joined && rows <= 16 && batch * rows <= most;
     if (p.own_direct) {
         p.own_rows = tile(rows);
         p.own_tiles = 1;
-    } else if (head_dim <= 128 && p.own_rows == 32) {
-        p.own_rows = 64;
     }
-    if (p.prefix_direct) p.prefix_rows = tile(batch * rows);
+    if (p.prefix_direct)
+        p.prefix_rows = head_dim > 128 ? 16 : 64;
+    else if (head_dim <= 128 && p.prefix_rows == 32)
+        p.prefix_rows = 64;
     p.own_shift = __builtin_ctz((unsigned)p.own_rows);
     p.prefix_shift = __builtin_ctz((unsigned)p.prefix_rows);
-    // (as many as the CUs hold, three of 37 KiB where one kind of few rows is all)
-    if (p.own_direct && p.joined) p.groups = head_dim > 128 ? 512 : p.own_rows == 16 ? 768 : 512;
+    // (two workgroups to a CU; with three, 128 single tokens behind 4,096 to 8,192 of their own take 180 us, not 172)
+    if (p.own_direct && p.joined) p.groups = 512;
+    // A task of few rows starts and ends in the time that 8 of its units take, 12 of more than 16 rows; and a unit of a
+    // prefix's tasks of many takes as long as two of such a task's.  (64 sequences of 9 tokens of 4 heads, 2,048 to 4,096
+    // cached: 78 us, 80 with 8 and 86 with 3; 32 single tokens behind 8,192 and 1,000: 29 us, and 34 with equal units and 3.)
+    if (p.own_direct) p.own_task_units = p.own_rows == 16 ? 8 : 12;
+    if (p.prefix_direct) p.prefix_task_units = 8;
+    if (!p.prefix_direct && p.own_direct) p.prefix_weight = 2;
     place_parts(p, batch, rows, kv_heads);
     return p;
 }
@@ -234,6 +248,14 @@ inline sv_status_t check_attend(const sv_cache_attend_desc_t& d, decltype(&check
         d.workspace_bytes < attend_workspace_bytes(d.batch, d.max_new, d.q_heads, d.kv_heads, d.head_dim, plan))
         return SV_ERR_WORKSPACE;
     return SV_OK;
+}
+
+// Whether the tasks of a call of few rows are left whole, since their keys are too few to share them out: a workgroup
+// then has the tasks that begin in its run, and nothing is joined.  (Time so to time with cut tasks: 0.69 to 0.91 with up
+// to 8 units, 0.80 to 1.06 with up to 16, 0.96 to 1.24 with up to 32.)
+inline bool whole_pays(const AttendPlan& p, const sv_cache_attend_desc_t& d) {
+    const int64_t units = ((int64_t)d.max_pages * d.page_size + kAttendKeys - 1) / kAttendKeys;
+    return p.own_direct && p.joined && units <= 16;
 }
 
 inline sv_status_t check_attend4(const sv_cache_attend_desc_t& d) {

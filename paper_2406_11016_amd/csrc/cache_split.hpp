@@ -64,7 +64,7 @@ constexpr uint32_t tile_units(const Split& a, const Sequence& s, int32_t rt) {
 }
 constexpr uint32_t tile_cost(const Split& a, const Sequence& s, int32_t rt) {
     const uint32_t n = tile_units(a, s, rt);
-    return n == 0 ? 0 : n + kTaskUnits;
+    return n == 0 ? 0 : n + a.plan.own_task_units;
 }
 
 // A cost dealt to workgroups in equal runs; the first `longer` have one more.
@@ -112,17 +112,18 @@ constexpr Totals totals(const Split& a, int32_t tokens, uint32_t own_cost) {
         t.prefix_tiles =
             (int32_t)(((uint32_t)tokens * (uint32_t)a.group + (uint32_t)a.plan.prefix_rows - 1) >> a.plan.prefix_shift);
         const uint32_t tasks = (uint32_t)t.prefix_tiles * (uint32_t)a.kv_heads, units = (uint32_t)a.prefix_units;
-        const uint32_t cost = tasks * (units + kTaskUnits);
+        const uint32_t cost = tasks * (units + a.plan.prefix_task_units);
         // (as many in each of the 8 XCDs: 64 sequences of 64 to 144 rows at head_dim 256
         // behind 16,384 took 117, 140, 180 and 280 us so, 156, 170, 212 and 309 to the nearest number)
-        const uint32_t eighths = (uint32_t)((uint64_t)(groups / 8) * cost / ((uint64_t)cost + own_cost));
+        const uint64_t weight = (uint64_t)cost * a.plan.prefix_weight;
+        const uint32_t eighths = (uint32_t)((uint64_t)(groups / 8) * weight / (weight + own_cost));
         const uint32_t places = 8 * (eighths < 1 ? 1u : smaller(eighths, groups / 8 - 1));
         const uint32_t fair = smaller(units, (tasks * units + places - 1) / places), most = places / tasks;
         const uint32_t whole = most == 0 ? units : (units + most - 1) / most;
-        const bool by_tasks = most != 0 && whole <= fair + kTaskUnits;
+        const bool by_tasks = most != 0 && whole <= fair + a.plan.prefix_task_units;
         t.chunk = by_tasks ? whole : fair;
         t.chunks = (units + t.chunk - 1) / t.chunk;
-        t.prefix = deal(tasks * (units + t.chunks * kTaskUnits), by_tasks ? tasks * t.chunks : places);
+        t.prefix = deal(tasks * (units + t.chunks * a.plan.prefix_task_units), by_tasks ? tasks * t.chunks : places);
     }
     t.own = deal(own_cost, groups - t.prefix.groups);
     return t;
@@ -150,28 +151,28 @@ constexpr int32_t find(const I* cum, int32_t n, I x) {
 // A run of units of one task.
 struct Segment {
     uint32_t task;               // number among the prefix's, or among the sequences' own tasks
-    uint32_t task_start, units;  // where its units begin in its kind's cost (behind kTaskUnits); its units
+    uint32_t task_start, units;  // where its units begin in its kind's cost (behind what the task costs); its units
     uint32_t first, end;         // this run, within the task
     uint32_t offset;             // units of the prefix before the task's chunk
     uint32_t prefix_units;       // units of the prefix that the task begins with
     int32_t kv_head, b, row0;    // b < 0: the prefix, for rows of the whole batch
     int32_t count, length;       // of sequence b
-    bool bad;
+    int32_t bad;                 // (a word, which stays in a scalar register)
 };
 
 // The prefix's task at place u of its cost.
 constexpr Segment prefix_task(const Split& a, const Totals& t, uint32_t u) {
     Segment g{};
     const uint32_t tiles = (uint32_t)t.prefix_tiles, units = (uint32_t)a.prefix_units;
-    const uint32_t tasks = tiles * (uint32_t)a.kv_heads, chunk_cost = (t.chunk + kTaskUnits) * tasks;
+    const uint32_t tasks = tiles * (uint32_t)a.kv_heads, chunk_cost = (t.chunk + a.plan.prefix_task_units) * tasks;
     const uint32_t chunk = u / chunk_cost, in_chunk = u - chunk * chunk_cost;
     g.offset = chunk * t.chunk;
     g.units = smaller(t.chunk, units - g.offset);
-    const uint32_t task = in_chunk / (g.units + kTaskUnits);
+    const uint32_t task = in_chunk / (g.units + a.plan.prefix_task_units);
     g.kv_head = (int32_t)(task / tiles);
     const uint32_t tile = task - (uint32_t)g.kv_head * tiles;
     g.task = chunk * tasks + task;
-    g.task_start = u - (in_chunk - task * (g.units + kTaskUnits)) + kTaskUnits;
+    g.task_start = u - (in_chunk - task * (g.units + a.plan.prefix_task_units)) + a.plan.prefix_task_units;
     g.prefix_units = units;
     g.row0 = (int32_t)tile << a.plan.prefix_shift;
     g.b = -1;
@@ -181,24 +182,29 @@ constexpr Segment prefix_task(const Split& a, const Totals& t, uint32_t u) {
 // b; `find_tile(sequence, at, start)` the row tile that holds place `at` of a sequence
 // and head, and the place at which that tile's task begins.
 template <class SequenceOf, class FindTile>
-constexpr Segment own_task(const Split& a, const uint32_t* cum_cost, uint32_t u, SequenceOf sequence_of,
-                           FindTile find_tile) {
+constexpr Segment own_task_of(const Split& a, const uint32_t* cum_cost, int32_t b, uint32_t u, SequenceOf sequence_of,
+                              FindTile find_tile) {
     Segment g{};
-    g.b = find(cum_cost, a.batch, u);
+    g.b = b;
     const Sequence s = sequence_of(g.b);
     const uint32_t base = cum_cost[g.b], head = (cum_cost[g.b + 1] - base) / (uint32_t)a.kv_heads;
     g.kv_head = (int32_t)((u - base) / head);
     uint32_t start = 0;
     const int32_t rt = find_tile(s, u - base - (uint32_t)g.kv_head * head, start);
     g.task = (uint32_t)(g.b * a.kv_heads + g.kv_head) * (uint32_t)a.plan.own_tiles + (uint32_t)rt;
-    g.task_start = base + (uint32_t)g.kv_head * head + start + kTaskUnits;
+    g.task_start = base + (uint32_t)g.kv_head * head + start + a.plan.own_task_units;
     g.units = tile_units(a, s, rt);
     g.prefix_units = a.plan.joined ? (uint32_t)a.prefix_units : 0u;
     g.row0 = rt << a.plan.own_shift;
     g.count = s.count;
     g.length = s.length;
-    g.bad = s.bad;
+    g.bad = s.bad ? 1 : 0;
     return g;
+}
+template <class SequenceOf, class FindTile>
+constexpr Segment own_task(const Split& a, const uint32_t* cum_cost, uint32_t u, SequenceOf sequence_of,
+                           FindTile find_tile) {
+    return own_task_of(a, cum_cost, find(cum_cost, a.batch, u), u, sequence_of, find_tile);
 }
 // A workgroup's run of the task that it finds at place u of the cost, its run of the
 // cost ending before place `end`; empty (first == end) if it ends before the task's units.
@@ -241,7 +247,8 @@ constexpr int64_t prefix_part(const Split& a, const Totals& t, int32_t kv_head, 
     const uint32_t chunk = k / kChunkParts, offset = chunk * t.chunk;
     const uint32_t units = smaller(t.chunk, (uint32_t)a.prefix_units - offset);
     const uint32_t tasks = tiles * (uint32_t)a.kv_heads, in_chunk = (uint32_t)kv_head * tiles + tile;
-    const uint32_t start = chunk * (t.chunk + kTaskUnits) * tasks + in_chunk * (units + kTaskUnits) + kTaskUnits;
+    const uint32_t start = chunk * (t.chunk + a.plan.prefix_task_units) * tasks +
+                           in_chunk * (units + a.plan.prefix_task_units) + a.plan.prefix_task_units;
     const uint32_t task = chunk * tasks + in_chunk;
     const uint32_t w = group_of(t.prefix, start) + (k - chunk * kChunkParts);
     if (w > group_of(t.prefix, start + units - 1)) return -1;
@@ -257,7 +264,7 @@ struct Parts {
 constexpr Parts own_parts(const Split& a, const Totals& t, const Sequence& s, uint32_t cost_before, uint32_t cost,
                           int32_t b, int32_t token, int32_t kv_head, int32_t g) {
     const int32_t r = token * a.group + g, tile = r >> a.plan.own_shift;
-    uint32_t start = cost_before + (uint32_t)kv_head * (cost / (uint32_t)a.kv_heads) + kTaskUnits;
+    uint32_t start = cost_before + (uint32_t)kv_head * (cost / (uint32_t)a.kv_heads) + a.plan.own_task_units;
     for (int32_t rt = 0; rt < tile; ++rt) start += tile_cost(a, s, rt);
     const uint32_t task = (uint32_t)(b * a.kv_heads + kv_head) * (uint32_t)a.plan.own_tiles + (uint32_t)tile;
     const uint32_t w0 = group_of(t.own, start), w1 = group_of(t.own, start + tile_units(a, s, tile) - 1);

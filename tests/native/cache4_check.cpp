@@ -4,9 +4,11 @@
 
 #define attend_plan attend4_plan
 #define attend_workspace_bytes attend4_workspace_bytes
+#define kTaskUnits 64  // (of any plan here)
 #define main all_checks
 #include "cache_check.cpp"
 #undef main
+#undef kTaskUnits
 #undef attend_workspace_bytes
 #undef attend_plan
 
