@@ -590,9 +590,12 @@ struct Work {
             if (16 * R::kHalves % 64 != 0 && at >= 16 * R::kHalves) continue;
             const int r = at / R::kHalves, half = at % R::kHalves;
             const float by = __uint_as_float(scale[j] << 23);
+            // (of 8 lanes four write their even chunk first and four their odd one: on all banks together)
+            const int flip = (S::kPitch == 64 ? r : half >> 2) & 1;
 #pragma unroll
             for (int i = 0; i < 2; ++i)
-                *(u32x4*)(to + r * (S::kPitch * 2) + (((2 * half + i) ^ swizzle<D>(r)) * 16)) = T::wide(codes[j][i], by);
+                *(u32x4*)(to + r * (S::kPitch * 2) + (((2 * half + (i ^ flip)) ^ swizzle<D>(r)) * 16)) =
+                    T::wide(flip != 0 ? codes[j][1 - i] : codes[j][i], by);
         }
     }
     __device__ __forceinline__ void stage_first() {

@@ -300,7 +300,7 @@ def _dtype4(what: str, dtype) -> int:
 
 def append4(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, slots: torch.Tensor) -> None:
     """append() to caches in 4 bits (uint8; see PagedCache.new_storage): ``k`` and ``v [B, n, kv_heads, head_dim]`` are
-    quantised as they are written (spec_cache_append4)."""
+    quantised as they are written (spec_cache_append4).  The page size follows from a page's bytes and head_dim."""
     lib = _lib if _lib is not None else load_library()
     shape, dtype = k.shape, k.dtype
     if len(shape) != 4:
