@@ -209,8 +209,8 @@ size_t spec_cache_attend_workspace_bytes(int32_t batch, int32_t max_new, int32_t
  * 3.5 .. 7, but not below 2^-23 (fp16) or 2^-125 (bf16), so that what is held are
  * numbers of the storage type.  Values go to the nearest number that the codes have,
  * those in the middle of two to the even code, those beyond 6 to 6: they move by
- * at most a sixth of the block's largest magnitude.  A block with an infinity or NaN
- * reads as NaN.
+ * at most a fifth of the block's largest magnitude, or a quarter of the smallest
+ * scale where that is more.  A block with an infinity or NaN reads as NaN.
  */
 sv_status_t spec_cache_append4(const sv_cache_append_desc_t* desc, hipStream_t stream);
 

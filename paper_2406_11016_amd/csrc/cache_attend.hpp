@@ -1,5 +1,6 @@
 // Attention of a step's new tokens to the paged cache, behind a prefix that the
-// batch shares, for gfx950 (MI355X): kernels of spec_cache_attend.
+// batch shares, for gfx950 (MI355X): kernels of spec_cache_attend, and the tasks of many
+// rows and the joining kernels of spec_cache_attend4.
 // (Included by the sources of the two storage types.)
 //
 // Work is cut into tasks of up to 128 query rows of one key/value head (a row
