@@ -206,11 +206,14 @@ size_t spec_cache_attend_workspace_bytes(int32_t batch, int32_t max_new, int32_t
  * spec_cache_append to such caches: each token's values are quantised as they
  * are written, by themselves, so nothing that was written before changes.  A
  * block's scale is the power of two that brings its largest magnitude into
- * 3.5 .. 7, but not below 2^-23 (fp16) or 2^-125 (bf16), so that what is held are
- * numbers of the storage type.  Values go to the nearest number that the codes have,
- * those in the middle of two to the even code, those beyond 6 to 6: they move by
- * at most a fifth of the block's largest magnitude, or a quarter of the smallest
- * scale where that is more.  A block with an infinity or NaN reads as NaN.
+ * 3.5 .. 7, but not below 2^-23 (fp16) or 2^-125 (bf16).  Values go to the nearest number
+ * that the codes have, those in the middle of two to the even code, those beyond 6 to 6:
+ * they move by at most a fifth of the block's largest magnitude, or a quarter of the
+ * smallest scale where that is more.  With the greatest scale, 2^14 (fp16, a largest
+ * magnitude of 57,344 or more) or 2^126 (bf16, 1.75 * 2^127 or more), 4 is no number of the
+ * storage type, and those of 3.5 and more go to 3: they move by at most a quarter of the
+ * largest.  So what is held of finite values are finite numbers of the storage type.
+ * A block with an infinity or NaN reads as NaN.
  */
 sv_status_t spec_cache_append4(const sv_cache_append_desc_t* desc, hipStream_t stream);
 

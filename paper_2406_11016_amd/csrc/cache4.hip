@@ -18,9 +18,10 @@ typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 // The storage types: a magnitude as fp32, and two values to and from 4 bits each (byte
-// `kByte` of the codes) with a scale, whose exponent counts.
+// `kByte` of the codes) with a scale, whose exponent counts.  kLast (twice): the last number
+// before 3.5 times the greatest scale.
 struct Half {
-    static constexpr uint32_t kNotFinite = 0x7c00, kLeast = kPackedLeastF16;
+    static constexpr uint32_t kNotFinite = 0x7c00, kLeast = kPackedLeastF16, kLast = 0x7aff7affu;
     static __device__ __forceinline__ float value(uint32_t bits) {
         return (float)__builtin_bit_cast(_Float16, (uint16_t)bits);
     }
@@ -34,7 +35,7 @@ struct Half {
     }
 };
 struct BFloat {
-    static constexpr uint32_t kNotFinite = 0x7f80, kLeast = kPackedLeastBF16;
+    static constexpr uint32_t kNotFinite = 0x7f80, kLeast = kPackedLeastBF16, kLast = 0x7f5f7f5fu;
     static __device__ __forceinline__ float value(uint32_t bits) { return __uint_as_float(bits << 16); }
     template <int kByte>
     static __device__ __forceinline__ uint32_t pack(uint32_t codes, uint32_t two, float scale) {
@@ -48,6 +49,12 @@ struct BFloat {
 
 __device__ __forceinline__ uint32_t max_pair(uint32_t x, uint32_t y) {
     return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, x), __builtin_bit_cast(u16x2, y)));
+}
+// Two values whose magnitudes are `last` at most.
+__device__ __forceinline__ uint32_t within(uint32_t two, uint32_t last) {
+    const uint32_t m = __builtin_bit_cast(uint32_t, __builtin_elementwise_min(__builtin_bit_cast(u16x2, two & 0x7fff7fffu),
+                                                                              __builtin_bit_cast(u16x2, last)));
+    return m | (two & 0x80008000u);
 }
 // The largest magnitude (its bits) of 8 values, and of the 32 that four neighbouring lanes
 // have: magnitudes are ordered as their bits, with infinity and NaN on top.
@@ -64,17 +71,19 @@ __device__ __forceinline__ uint32_t largest_of_four(uint32_t m) {
 
 // 8 values of a block whose largest magnitude is known: its scale's byte, and their codes.
 // The scale is the power of two that brings the magnitude into 3.5 .. 7: adding a
-// quarter of the mantissa's range carries into the exponent from 1.75 on.
+// quarter of the mantissa's range carries into the exponent from 1.75 on.  The types have
+// no number of 4 times the greatest scale (fp16 2^14, bf16 2^126), so what would round to it, from
+// 3.5 on, goes to 3 times it; with smaller scales all numbers are below kLast.
 template <class T>
 __device__ __forceinline__ uint32_t quantise(const u32x4& x, uint32_t magnitude, uint32_t& byte) {
     const int exponent = (int)((__float_as_uint(T::value(magnitude)) + 0x200000u) >> 23) - 2;
     byte = (uint32_t)max(exponent, (int)T::kLeast);
     if (magnitude >= T::kNotFinite) byte = kPackedNaN;
     const float scale = __uint_as_float(byte << 23);
-    uint32_t codes = T::template pack<0>(0u, x[0], scale);
-    codes = T::template pack<1>(codes, x[1], scale);
-    codes = T::template pack<2>(codes, x[2], scale);
-    codes = T::template pack<3>(codes, x[3], scale);
+    uint32_t codes = T::template pack<0>(0u, within(x[0], T::kLast), scale);
+    codes = T::template pack<1>(codes, within(x[1], T::kLast), scale);
+    codes = T::template pack<2>(codes, within(x[2], T::kLast), scale);
+    codes = T::template pack<3>(codes, within(x[3], T::kLast), scale);
     return byte == kPackedNaN ? 0u : codes;
 }
 

@@ -15,7 +15,8 @@ constexpr int packed_blocks(int head_dim) { return (head_dim + kPackedBlock - 1)
 constexpr int packed_row(int head_dim) { return head_dim / 2 + packed_blocks(head_dim); }
 
 // The smallest scales' bytes (exponent + 127): half of such a scale is the smallest number
-// of fp16, the smallest normal one of bf16.  So whatever is held is a number of the type.
+// of fp16, the smallest normal one of bf16.  So whatever is held is a number of the type
+// (with the greatest scales, what is written is 3 times the scale at most: see quantise()).
 constexpr uint32_t kPackedLeastF16 = 127 - 23;
 constexpr uint32_t kPackedLeastBF16 = 127 - 125;
 constexpr uint32_t kPackedNaN = 255;

@@ -6,6 +6,7 @@ from tests.cache_util import TORCH_DTYPES
 
 BLOCK = 32
 LEAST = {torch.float16: -23, torch.bfloat16: -125}
+GREATEST = {torch.float16: 14, torch.bfloat16: 126}  # 4 times such a scale is not a number of the type
 NUMBERS = np.array([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0])
 
 
@@ -32,6 +33,7 @@ def quantise(x):
         # the nearest number; of two as near the one with the even code
         off = np.abs(y[..., None] - NUMBERS)
         off = off + np.where(np.arange(8) % 2 == 1, 1e-12, 0.0) * 1.0
+        off = np.where((e[..., None, None] == GREATEST[x.dtype]) & (NUMBERS >= 4.0), np.inf, off)
         code = off.argmin(-1) + 8 * np.signbit(block)
         codes[..., i * BLOCK:(i + 1) * BLOCK] = np.where(finite[..., None], code, 0)
         scales[..., i] = np.where(finite, e + 127, 255)
