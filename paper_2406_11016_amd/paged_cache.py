@@ -270,7 +270,19 @@ def row_bytes4(head_dim: int) -> int:
     return head_dim // 2 + (head_dim + 31) // 32
 
 
-def _caches4(k_cache: torch.Tensor, v_cache: torch.Tensor, head_dim: int):
+def _page4(size: int, head_dim: int, page_size: Optional[int]) -> int:
+    """Tokens of a page that has ``size`` bytes a head: ``page_size`` of them, where that is given."""
+    row = row_bytes4(head_dim)
+    if size % row:
+        raise SpecVerifyError(f"{size} bytes of a page and head are no whole number of tokens of {row} bytes "
+                              f"(head_dim {head_dim})")
+    if page_size is not None and size != page_size * row:
+        raise SpecVerifyError(f"{size} bytes of a page and head are {size // row} tokens of head_dim {head_dim}, not "
+                              f"page_size={page_size}")
+    return size // row
+
+
+def _caches4(k_cache: torch.Tensor, v_cache: torch.Tensor, head_dim: int, page_size: Optional[int]):
     """A pair of caches in 4 bits: device, pages, heads, page size, addresses and the stride of their pages in bytes."""
     index, shape, strides = k_cache.get_device(), k_cache.shape, k_cache.stride()
     if index < 0 or len(shape) != 3 or k_cache.dtype != torch.uint8:
@@ -279,16 +291,13 @@ def _caches4(k_cache: torch.Tensor, v_cache: torch.Tensor, head_dim: int):
             v_cache.stride() != strides:
         raise SpecVerifyError("k_cache and v_cache must be alike in shape, strides, dtype and device")
     (n, h, size), (sn, sh, sb) = shape, strides
-    row = row_bytes4(head_dim)
-    if size % row:
-        raise SpecVerifyError(f"{size} bytes of a page and head are no whole number of tokens of {row} bytes "
-                              f"(head_dim {head_dim})")
+    page = _page4(size, head_dim, page_size)
     if n == 1:
         sn = max(sn, h * size)
     k, v = k_cache.data_ptr(), v_cache.data_ptr()
     if sb != 1 or (h > 1 and sh != size) or (sn | k | v) & 15:
         raise SpecVerifyError("a cache's pages must be dense and aligned to 16 bytes")
-    return index, n, h, size // row, k, v, sn
+    return index, n, h, page, k, v, sn
 
 
 def _dtype4(what: str, dtype) -> int:
@@ -298,16 +307,19 @@ def _dtype4(what: str, dtype) -> int:
     return code
 
 
-def append4(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, slots: torch.Tensor) -> None:
+def append4(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, slots: torch.Tensor, *,
+            page_size: Optional[int] = None) -> None:
     """append() to caches in 4 bits (uint8; see PagedCache.new_storage): ``k`` and ``v [B, n, kv_heads, head_dim]`` are
-    quantised as they are written (spec_cache_append4).  The page size follows from a page's bytes and head_dim."""
+    quantised as they are written (spec_cache_append4).  The page size follows from a page's bytes and head_dim, and a
+    cache that was made for another head_dim may fit in pages of another size: with ``page_size`` it is refused (as by
+    PagedCache's methods, and so for read4() and attend4())."""
     lib = _lib if _lib is not None else load_library()
     shape, dtype = k.shape, k.dtype
     if len(shape) != 4:
         raise SpecVerifyError(f"k and v must be [batch, tokens, kv_heads, head_dim]; k is {list(shape)}")
     B, n, H, d = shape
     code = _dtype4("k and v", dtype)
-    index, num_pages, h, p, k_at, v_at, page_stride = _caches4(k_cache, v_cache, d)
+    index, num_pages, h, p, k_at, v_at, page_stride = _caches4(k_cache, v_cache, d, page_size)
     if H != h:
         raise SpecVerifyError(f"k and v must have {h} heads for these caches; k is {list(shape)}")
     k_from, kb, kt, kh = _rows("k", k, shape, index, dtype)
@@ -319,12 +331,13 @@ def append4(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: to
 
 
 def read4(k_cache: torch.Tensor, v_cache: torch.Tensor, slots: torch.Tensor, head_dim: Optional[int] = None, dtype=None, *,
-          out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+          out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None,
+          page_size: Optional[int] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """Keys and values of the slots that ``slots`` (int32 ``[B, n]``) names, back from caches in 4 bits.
 
     Returns ``(k, v)``, ``[B, n, kv_heads, head_dim]`` of ``dtype`` (float16 or bfloat16, what they were written from).
     Rows whose slot is outside the cache (-1) are not written; new tensors are zero there.  ``out`` gives the tensors,
-    and head_dim and dtype with them; they do not overlap.
+    and head_dim and dtype with them; they do not overlap.  ``page_size``: see append4().
     """
     lib = _lib if _lib is not None else load_library()
     if slots.dim() != 2:
@@ -341,7 +354,7 @@ def read4(k_cache: torch.Tensor, v_cache: torch.Tensor, slots: torch.Tensor, hea
         raise SpecVerifyError(f"out must be two tensors [batch, tokens, kv_heads, head_dim]; the first is {k.dtype} "
                               f"{list(shape)}")
     d, code = shape[3], _dtype4("out", k.dtype)
-    index, num_pages, h, p, k_at, v_at, page_stride = _caches4(k_cache, v_cache, d)
+    index, num_pages, h, p, k_at, v_at, page_stride = _caches4(k_cache, v_cache, d, page_size)
     k_to, kb, kt, kh = _rows("out[0]", k, (B, n, h, d), index, k.dtype)
     v_to, vb, vt, vh = _rows("out[1]", v, (B, n, h, d), index, k.dtype)
     _int32("slots", slots, (B, n), index)
@@ -368,14 +381,16 @@ def new_attend4_workspace(batch: int, max_new: int, q_heads: int, kv_heads: int,
 def attend4(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, block_table: torch.Tensor,
             lengths: torch.Tensor, counts: Optional[torch.Tensor] = None, *,
             prefix_table: Optional[torch.Tensor] = None, prefix_len: int = 0, scale: Optional[float] = None,
-            out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+            out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+            page_size: Optional[int] = None) -> torch.Tensor:
     """attend() over caches in 4 bits: of the values that read4() gives for q's type.  All else is as there, but that at
-    head_dim 256 the batch is at most 1,024; the ``workspace`` is new_attend4_workspace()'s."""
+    head_dim 256 the batch is at most 1,024; the ``workspace`` is new_attend4_workspace()'s.  ``page_size``: see
+    append4()."""
     lib = _lib if _lib is not None else load_library()
     if q.dim() != 4:
         raise SpecVerifyError(f"q must be [batch, tokens, q_heads, head_dim]; it is {list(q.shape)}")
     _dtype4("q", q.dtype)
-    index, num_pages, K, P, k_at, v_at, page_stride = _caches4(k_cache, v_cache, q.shape[3])
+    index, num_pages, K, P, k_at, v_at, page_stride = _caches4(k_cache, v_cache, q.shape[3], page_size)
     return _attend(lib.spec_cache_attend4, "spec_cache_attend4", new_attend4_workspace, q, index, q.dtype, num_pages, K, P,
                    k_at, v_at, page_stride, block_table, lengths, counts, prefix_table, prefix_len, scale, out, workspace)
 
