@@ -270,8 +270,14 @@ def row_bytes4(head_dim: int) -> int:
     return head_dim // 2 + (head_dim + 31) // 32
 
 
+def _head_dim4(head_dim: int) -> None:
+    if head_dim < 8 or head_dim % 8:
+        raise SpecVerifyError(f"head_dim must be a multiple of 8; got {head_dim}")
+
+
 def _page4(size: int, head_dim: int, page_size: Optional[int]) -> int:
     """Tokens of a page that has ``size`` bytes a head: ``page_size`` of them, where that is given."""
+    _head_dim4(head_dim)
     row = row_bytes4(head_dim)
     if size % row:
         raise SpecVerifyError(f"{size} bytes of a page and head are no whole number of tokens of {row} bytes "
@@ -347,6 +353,7 @@ def read4(k_cache: torch.Tensor, v_cache: torch.Tensor, slots: torch.Tensor, hea
         if head_dim is None or k_cache.dim() != 3:
             raise SpecVerifyError("read4 needs head_dim and dtype, or out, and caches [num_pages, kv_heads, bytes of a page]")
         _dtype4("dtype", dtype)
+        _head_dim4(head_dim)
         out = tuple(torch.zeros(B, n, k_cache.shape[1], head_dim, dtype=dtype, device=k_cache.device) for _ in range(2))
     k, v = out
     shape = k.shape
