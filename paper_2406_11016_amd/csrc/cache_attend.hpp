@@ -437,20 +437,16 @@ struct Work {
             now.prefix_tiles = forget_scalar(now.prefix_tiles);
             g = uniform(prefix_task(a.split, now, at));
         } else if constexpr (C::kDirect) {  // (such tasks have all of a sequence's rows)
-            auto task = [&]() {
-                return uniform(own_task(a.split, batch.cum_cost, at, [&](int32_t b) { return sequence(batch, b); },
+            auto task_at = [&](uint32_t place) {
+                return uniform(own_task(a.split, batch.cum_cost, place, [&](int32_t b) { return sequence(batch, b); },
                                         [](const Sequence&, uint32_t, uint32_t& start) {
                                             start = 0;
                                             return 0;
                                         }));
             };
-            g = task();
-            if (kKind == kJoined && a.split.plan.whole_tasks) {  // the tasks that begin in this run, to their ends
-                if (at + a.split.plan.own_task_units > g.task_start) {
-                    at = g.task_start + g.units;
-                    if (at >= end) return false;
-                    g = task();
-                }
+            g = task_at(at);
+            if (kKind == kJoined && a.split.plan.whole_tasks) {
+                if (!to_whole_task(a.split, g, at, end, task_at)) return false;
                 to = g.task_start + g.units;
             }
         } else if constexpr (kKind == kShared)

@@ -213,6 +213,19 @@ constexpr void cut(Segment& g, uint32_t u, uint32_t end) {
     g.end = end > g.task_start ? smaller(g.units, end - g.task_start) : 0u;
 }
 
+// Where a call's tasks are left whole (AttendPlan::whole_tasks), a workgroup has those that begin in
+// its run of the cost.  `g` is the task at place `at` of it: one that began before `at` was
+// another's, and then `g` and `at` move to the next one (`task_at` gives the task at a place); false
+// if there is none before `end`.
+template <class TaskAt>
+constexpr bool to_whole_task(const Split& a, Segment& g, uint32_t& at, uint32_t end, TaskAt task_at) {
+    if (at + a.plan.own_task_units <= g.task_start) return true;
+    at = g.task_start + g.units;
+    if (at >= end) return false;
+    g = task_at(at);
+    return true;
+}
+
 // The keys of a unit that a wave stages are a run of 16, which lies within a page.
 // Run r (0 .. kAttendKeys / 16 - 1) of a unit that begins at key `base`: its
 // first key; behind the last key there is, the run that holds it.
