@@ -1327,8 +1327,12 @@ __global__ void __launch_bounds__(kThreads) attend_join_tasks_kernel(AttendArgs 
     const uint32_t w = blockIdx.x + 1;
     if (w >= t.own.groups) return;
     const uint32_t start = group_start(t.own, w);
+    // (find()'s loads, a halving each, against find_by_wave()'s two: the kernel takes 7.4 and 7.6 us for 8 sequences of 36 rows, 8.4 and
+    // 8.7 for 16, 9.8 and 9.8 for 32, 10.0 and 9.5 for 64, 10.4 and 9.1 for 300; of many rows 23.0 and 23.9 for 8, 17.5 and
+    // 18.4 for 32, 19.9 and 19.9 for 128)
+    const int32_t b = split.batch <= 32 ? find(a.cum_cost, split.batch, start) : find_by_wave(a.cum_cost, split.batch, start);
     const Segment g = uniform(own_task_of(
-        split, a.cum_cost, find_by_wave(a.cum_cost, split.batch, start), start, [&](int32_t b) { return sequence(split, b); },
+        split, a.cum_cost, b, start, [&](int32_t b) { return sequence(split, b); },
         [&](const Sequence& s, uint32_t at, uint32_t& tile_start) { return find_tile(split, s, at, tile_start); }));
     uint32_t w0, w1;
     if (!cuts_task(t, g, w, w0, w1)) return;
