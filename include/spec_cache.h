@@ -191,7 +191,7 @@ size_t spec_cache_attend_workspace_bytes(int32_t batch, int32_t max_new, int32_t
  * Caches in 4 bits.  A value is held as an e2m1 number (0, 0.5, 1, 1.5, 2, 3, 4, 6
  * and their negatives: codes 0 to 7, and 8 to 15), and each block of 32 values of a
  * token and head (head_dim's last block may be shorter) shares a power of two,
- * whose exponent + 127 is a byte: 4.25 bits a value.  This is the block format of
+ * whose exponent + 127 is a byte: 4.25 bits a value (4.3 at head_dim 80).  This is the block format of
  * the OCP microscaling specification (MXFP4), so the byte 255 makes its block NaN.
  *   k_cache, v_cache  [num_pages, kv_heads, page_size * row] bytes, with
  *                     row = head_dim / 2 + (head_dim + 31) / 32.  Of each page and
@@ -244,7 +244,9 @@ sv_status_t spec_cache_read4(const sv_cache_read_desc_t* desc, hipStream_t strea
  * spec_cache_read4 gives for `dtype`, with the same accuracy, limits and errors, but for at
  * most SV_CACHE4_MAX_BATCH_D256 sequences at head_dim 256.  (Values
  * that do not fit fp16, as bf16 may have written them, are infinite or lose
- * bits there.)
+ * bits there.)  Without a prefix, for up to 48 rows (tokens x q_heads / kv_heads; 16 at
+ * head_dim 256) and tables of up to 1,024 tokens a sequence, it is one launch, two otherwise:
+ * a table no larger than the sequences need saves short ones 3 us.
  */
 sv_status_t spec_cache_attend4(const sv_cache_attend_desc_t* desc, hipStream_t stream);
 

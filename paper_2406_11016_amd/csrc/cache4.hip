@@ -102,7 +102,7 @@ __device__ __forceinline__ Place place_of(uint32_t slot, uint32_t head, int64_t 
 
 // A thread has 8 values of K and of V, and four threads a block of 32 (head_dim is filled up
 // to whole blocks by threads without values).  Bound by memory: 9,032 tokens of 8 heads of 128,
-// 37 MB in and 10 out, 12.0 us, 3.9 TB/s; 447 tokens 3.1 us, the latency of a launch and two loads.
+// 37 MB in and 10 out, 13.1 us, 3.6 TB/s; 447 tokens 3.4 us, the latency of a launch and two loads.
 template <class T>
 __global__ void __launch_bounds__(256) cache_append4_kernel(sv_cache_append_desc_t d, uint32_t chunks_head,
                                                             uint32_t chunks_token, int32_t page_shift, uint32_t total) {
@@ -139,7 +139,7 @@ __global__ void __launch_bounds__(256) cache_append4_kernel(sv_cache_append_desc
 }
 
 // A thread has 8 values of K and of V.  Bound by memory, most of it writes: 16,196 tokens of 8 heads of
-// 128, 18 MB in and 66 out, 17.1 us, 4.9 TB/s.  (Two to eight tokens a thread, tokens in the order of the pages
+// 128, 18 MB in and 66 out, 18.2 us, 4.6 TB/s.  (Two to eight tokens a thread, tokens in the order of the pages
 // and no divisions took 19.5 to 22.6 us, and this 20.4, called from Python.)
 template <class T>
 __global__ void __launch_bounds__(256) cache_read4_kernel(sv_cache_read_desc_t d, uint32_t chunks_head, uint32_t chunks_token,

@@ -3,9 +3,9 @@
 // (Included by cache4_attend.hpp; the split of the work is cache_attend.hpp's.)
 //
 // What it reaches, at head_dim 128: 128 sequences of 4 rows behind 4,096 to 8,192 keys,
-// 854 MB, 163 us (5.2 TB/s); 64 of 36 rows behind 2,048 to 4,096, 222 MB, 74 us, of which a
+// 854 MB, 167 us (5.1 TB/s); 64 of 36 rows behind 2,048 to 4,096, 222 MB, 70 us.  (Of 77, in a process's first calls, a
 // workgroup's units take 43 (5.1 TB/s) and starts and ends the others: the batch's sums 2, the
-// first task, its page, Q and its first loads 6, a task's end and the next one's start 7.
+// first task, its page, Q and its first loads 6, a task's end and the next one's start 7.)
 // With the keys in the L2, 16, 32 and 48 rows run at 530, 745 and 890 to 960 TFLOP/s.
 #pragma once
 

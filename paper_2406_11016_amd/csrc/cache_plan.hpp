@@ -86,7 +86,7 @@ struct AttendPlan {
     // only tasks cut by a workgroup's border have parts.  Otherwise the prefix
     // has tasks of its own, for the rows of the whole batch.
     bool joined;
-    int32_t own_rows, own_tiles;  // rows of a sequence's own task (32, 64 or 128); tasks a key/value head
+    int32_t own_rows, own_tiles;  // rows of a sequence's own task (32, 64 or 128; direct 16 too); tasks a key/value head
     int32_t prefix_rows;          // rows of a prefix task
     int32_t own_shift, prefix_shift;  // their logarithms
     int32_t groups;               // workgroups
@@ -209,7 +209,9 @@ inline AttendPlan attend4_plan(int32_t batch, int32_t max_new, int32_t q_heads, 
     if (p.own_direct && p.joined) p.groups = 512;
     // A task of few rows starts and ends in the time that 8 of its units take, 12 of more than 16 rows; and a unit of a
     // prefix's tasks of many takes as long as two of such a task's.  (64 sequences of 9 tokens of 4 heads, 2,048 to 4,096
-    // cached: 78 us, 80 with 8 and 86 with 3; 32 single tokens behind 8,192 and 1,000: 29 us, and 34 with equal units and 3.)
+    // cached: 78 us, 80 with 8 and 86 with 3; 32 single tokens behind 8,192 and 1,000: 29 us, and 34 with equal units and 3.
+    // With a prefix's unit as 1, 2, 3 and 4 of the others 64 sequences behind 16,384 take, of 36 rows, 190, 168, 173 and 173 us, of 28
+    // 158, 144, 137 and 137, of 8 64, 68, 62 and 61; behind 8,192 at head_dim 64, of 5, 71, 51, 49 and 52, at 256, of 4, 94, 77, 72 and 73.)
     if (p.own_direct) p.own_task_units = p.own_rows == 16 ? 8 : 12;
     if (p.prefix_direct) p.prefix_task_units = 8;
     if (!p.prefix_direct && p.own_direct) p.prefix_weight = 2;
