@@ -283,7 +283,7 @@ __device__ __forceinline__ void run_direct(const AttendArgs& a, const Totals& t,
         const int last = work.last_key(kKind == kShared);  // the last key that there is
 
         // ---- a unit's work
-        auto look_far = [&](int r) { far[r] = __any(fabsf(top[r] * a.scale_log2) > kFarScores && top[r] != -INFINITY); };
+        auto look_far = [&](int r) { far[r] = fabsf(top[r] * a.scale_log2) > kFarScores && top[r] != -INFINITY; };
         auto compute = [&](uint32_t u, int buffer, const KeysComing<D>& k, const uint32_t(&vs_in)[2], auto after_scores) {
             const int key0 = (int)u * kKeys;
             const bool partial = key0 + kKeys > (kKind == kShared ? a.prefix_len : own_first);
@@ -342,10 +342,13 @@ __device__ __forceinline__ void run_direct(const AttendArgs& a, const Totals& t,
                 for (int n = 0; n < 4; ++n)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) most = fmaxf(most, w[r][n][i]);
-                // (as in the 16-bit kernels: the weights' reference follows the maximum where it rises by more than 2^8)
+                // (as in the 16-bit kernels: the weights' reference follows the maximum where it rises by more than 2^8, row by row, so
+                // that keys which only other rows see change nothing)
                 if (__any(most - top[r] > a.lazy)) {
-                    const float now = fmaxf(top[r], quarters_max(most));
-                    const float by = now == -INFINITY ? 1.0f : exp2_hw((top[r] - now) * a.scale_log2);
+                    most = quarters_max(most);
+                    const bool rises = most - top[r] > a.lazy;
+                    const float now = rises ? most : top[r];
+                    const float by = rises ? exp2_hw((top[r] - now) * a.scale_log2) : 1.0f;
                     sum[r] *= by;
 #pragma unroll
                     for (int p = 0; p < S::kPieces; ++p) {
@@ -355,8 +358,8 @@ __device__ __forceinline__ void run_direct(const AttendArgs& a, const Totals& t,
                     top[r] = now;
                     look_far(r);
                 }
-                if (far[r]) {
-                    const float ref = top[r] == -INFINITY ? 0.0f : top[r];
+                if (__any(far[r])) {
+                    const float ref = far[r] ? top[r] : 0.0f;
 #pragma unroll
                     for (int n = 0; n < 4; ++n) w[r][n] -= ref;
                 }

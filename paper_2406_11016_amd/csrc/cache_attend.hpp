@@ -691,7 +691,7 @@ __device__ __forceinline__ bool segment(Work<C, D, kKind>& work, char* smem, flo
     }
     f32x16 o[kPieces];
     float top, sum = 0.0f;  // top: scores as they come from the product
-    bool far;               // some row's is beyond kFarScores: the scores of the unit at hand have lost it already
+    bool far;               // it is beyond kFarScores: the scores of the unit at hand have lost it already
 
     // Places of this lane's reads.  The swizzle flips bits of the chunk's number
     // only, so a read's constant part comes by an exclusive or (chunk) or as an
@@ -730,24 +730,24 @@ __device__ __forceinline__ bool segment(Work<C, D, kKind>& work, char* smem, flo
         return most;
     };
     // Whether, and then the scores without it.
-    auto look_far = [&]() {
-        far = __any(fabsf(top * a.scale_log2) > kFarScores && top != -INFINITY);
-    };
+    auto look_far = [&]() { far = fabsf(top * a.scale_log2) > kFarScores && top != -INFINITY; };
     auto take_off = [&](f32x16(&p)[NS]) {
-        if (!far) return;
-        const float ref = top == -INFINITY ? 0.0f : top;
+        if (!__any(far)) return;
+        const float ref = far ? top : 0.0f;
 #pragma unroll
         for (int s = 0; s < NS; ++s) p[s] -= ref;
     };
     // Moves the reference of the weights to unit u's maximum: they stay relative to a maximum of earlier units as
-    // long as the new one is within 2^8 of it, so nothing is rescaled for small rises.
+    // long as the new one is within 2^8 of it, so nothing is rescaled for small rises.  (Row by row, though the branch is the
+    // wave's: keys that only other rows see change nothing.)
     auto refer = [&](auto full, uint32_t u, f32x16(&p)[NS], float most) {
         if (!decltype(full)::value && partial_of(u)) most = mask(u, p);
         most = halves_max(most);
         // (the difference of two scores near one another is exact; next to a far one a.lazy would be rounded)
-        if (__any(most - top > a.lazy)) {
-            const float now = fmaxf(top, most);
-            const float by = (now == -INFINITY) ? 1.0f : exp2_hw((top - now) * a.scale_log2);
+        const bool rises = most - top > a.lazy;
+        if (__any(rises)) {
+            const float now = rises ? most : top;
+            const float by = rises ? exp2_hw((top - now) * a.scale_log2) : 1.0f;
             sum *= by;
 #pragma unroll
             for (int i = 0; i < kPieces; ++i) o[i] *= by;
